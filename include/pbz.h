@@ -81,7 +81,12 @@ typedef enum PBZ_ENUM {
   PBZ_ERR_HIP = -10,        /* the HIP runtime reported an error (no device, launch failure, ...) */
   PBZ_ERR_ALLOC = -11,      /* host allocation failed */
   PBZ_ERR_STATE = -12,      /* the call comes too late in the handle's life (see pbz_codec_set_transform) */
-  PBZ_ERR_CAPACITY = -13    /* the input exceeds what the library's fixed scratch array serves (pbz_segmented_static) */
+  PBZ_ERR_CAPACITY = -13,   /* the input exceeds what the library's fixed scratch array serves (pbz_segmented_static), or
+                               the caller's array is too short for the answer (pbz_pages_compact) */
+  PBZ_ERR_ALIGNMENT = -14,  /* a cache pool is not 16-byte aligned (pbz_cache.h) */
+  PBZ_ERR_PAGES = -15,      /* a page outside the pool or copied onto twice, or no free page left (pbz_cache.h) */
+  PBZ_ERR_SEQUENCE = -16,   /* no such sequence (pbz_cache.h) */
+  PBZ_ERR_MASK = -17        /* a cache's codec must not prune (pbz_cache.h) */
 } pbz_status;
 
 /* Kernel families, for pbz_codec_set_kernel_path / pbz_kernel_name. */

@@ -1,0 +1,341 @@
+"""Thin Python binding of the paged compressed cache (include/pbz_cache.h): keys and values of attention layers held as
+compressed arrays, attention taken on the compressed form, and the bookkeeping of pages.
+
+    cache = PagedCache(head_dim=128, heads=8, n_pages=1024, page_size=64)
+    seq = cache.open()
+    cache.extend_and_append([seq], [k.shape[0]], k, v)          # k, v: [tokens, heads, head_dim]
+    out = cache.attend_sequences([seq], [q.shape[0]], q)        # q: [tokens, query heads, head_dim]
+
+The calls on tensors (`append`, `attend`, `copy_pages`) take device tensors for slots, tables and lengths, allocate
+nothing but an output and a workspace where none is given, and can be captured into a graph with both given.  As in
+`api`, every step runs in the HIP kernels; there is no fallback.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import List, Optional, Sequence, Tuple
+
+import numpy as np
+
+from . import api
+
+_c = ctypes
+_p = _c.c_void_p
+_i64, _i32 = _c.c_int64, _c.c_int32
+
+
+class _Cache(_c.Structure):
+    _fields_ = [("n_pages", _i64), ("heads", _i32), ("page_size", _i32), ("k_N", _p), ("k_F", _p), ("v_N", _p), ("v_F", _p)]
+
+
+class _Lines(_c.Structure):
+    _fields_ = [("data", _p), ("token_stride", _i64), ("head_stride", _i64)]
+
+
+class _Attention(_c.Structure):
+    _fields_ = [("q", _p), ("out", _p), ("lse", _p), ("type", _c.c_int), ("q_heads", _i32), ("q_token_stride", _i64),
+                ("q_head_stride", _i64), ("out_token_stride", _i64), ("out_head_stride", _i64), ("n_tokens", _i64),
+                ("n_seqs", _i64), ("starts", _p), ("lengths", _p), ("table", _p), ("table_stride", _i64),
+                ("max_pages", _i64), ("max_new", _i64), ("max_length", _i64), ("causal", _i32), ("window", _i64),
+                ("scale", _c.c_float)]
+
+
+# name -> (restype, argtypes); mirrors include/pbz_cache.h declaration by declaration
+_i64p, _i32p, _sizep = _c.POINTER(_i64), _c.POINTER(_i32), _c.POINTER(_c.c_size_t)
+SIGNATURES = {
+    "pbz_cache_layout": (_c.c_int, [_p, _c.POINTER(_Cache), _sizep, _sizep]),
+    "pbz_cache_append": (_c.c_int, [_p, _c.POINTER(_Cache), _i64, _c.POINTER(_Lines), _c.POINTER(_Lines), _c.c_int, _p, _p]),
+    "pbz_cache_copy_pages": (_c.c_int, [_p, _c.POINTER(_Cache), _i64, _p, _p]),
+    "pbz_cache_attend_workspace": (_c.c_int, [_p, _c.POINTER(_Cache), _c.POINTER(_Attention), _sizep]),
+    "pbz_cache_attend": (_c.c_int, [_p, _c.POINTER(_Cache), _c.POINTER(_Attention), _p, _c.c_size_t, _p]),
+    "pbz_pages_create": (_c.c_int, [_c.POINTER(_p), _i64, _i32]),
+    "pbz_pages_destroy": (None, [_p]),
+    "pbz_pages_open": (_c.c_int, [_p, _i64p]),
+    "pbz_pages_fork": (_c.c_int, [_p, _i64, _i64p]),
+    "pbz_pages_close": (_c.c_int, [_p, _i64]),
+    "pbz_pages_extend": (_c.c_int, [_p, _i64, _i64, _p, _i32p, _i32p]),
+    "pbz_pages_truncate": (_c.c_int, [_p, _i64, _i64]),
+    "pbz_pages_length": (_c.c_int, [_p, _i64, _i64p, _i64p]),
+    "pbz_pages_table": (_c.c_int, [_p, _i64, _p, _i64]),
+    "pbz_pages_free_count": (_c.c_int, [_p, _i64p]),
+    "pbz_pages_compact": (_c.c_int, [_p, _p, _i64, _i64p]),
+}
+
+_declared = None
+
+
+def _library():
+    """libpbz.so with the cache's entry points declared."""
+    global _declared
+    lib = api.load_library()
+    if _declared is not lib:
+        for name, (res, args) in SIGNATURES.items():
+            fn = getattr(lib, name)
+            fn.restype = res
+            fn.argtypes = args
+        _declared = lib
+    return lib
+
+
+class Pages:
+    """Which sequence owns which page (pbz_pages): host-side, no device work.  Owns the handle."""
+
+    def __init__(self, n_pages: int, page_size: int):
+        self._lib = _library()
+        self._h = _p()
+        api.check(self._lib.pbz_pages_create(_c.byref(self._h), int(n_pages), int(page_size)))
+        self.n_pages, self.page_size = int(n_pages), int(page_size)
+
+    def __del__(self):
+        h, self._h = getattr(self, "_h", None), None
+        if h:
+            self._lib.pbz_pages_destroy(h)
+
+    def open(self) -> int:
+        seq = _i64()
+        api.check(self._lib.pbz_pages_open(self._h, _c.byref(seq)))
+        return seq.value
+
+    def fork(self, sequence: int) -> int:
+        seq = _i64()
+        api.check(self._lib.pbz_pages_fork(self._h, sequence, _c.byref(seq)))
+        return seq.value
+
+    def close(self, sequence: int) -> None:
+        api.check(self._lib.pbz_pages_close(self._h, sequence))
+
+    def extend(self, sequence: int, tokens: int) -> Tuple[np.ndarray, Optional[Tuple[int, int]]]:
+        """Slots (int64) of `tokens` more positions, and the (from, to) page copy to make before they are written."""
+        slots = np.empty(max(int(tokens), 1), dtype=np.int64)
+        copy, n = (_i32 * 2)(), _i32()
+        api.check(self._lib.pbz_pages_extend(self._h, sequence, int(tokens), slots.ctypes.data, copy, _c.byref(n)))
+        return slots, (copy[0], copy[1]) if n.value else None
+
+    def truncate(self, sequence: int, length: int) -> None:
+        api.check(self._lib.pbz_pages_truncate(self._h, sequence, int(length)))
+
+    def length(self, sequence: int) -> int:
+        n = _i64()
+        api.check(self._lib.pbz_pages_length(self._h, sequence, _c.byref(n), None))
+        return n.value
+
+    def table(self, sequence: int, capacity: Optional[int] = None) -> np.ndarray:
+        """The sequence's pages in order (int32), padded with -1 to `capacity`."""
+        if capacity is None:
+            n = _i64()
+            api.check(self._lib.pbz_pages_length(self._h, sequence, None, _c.byref(n)))
+            capacity = n.value
+        table = np.empty(max(int(capacity), 1), dtype=np.int32)
+        api.check(self._lib.pbz_pages_table(self._h, sequence, table.ctypes.data, int(capacity)))
+        return table[:capacity]
+
+    @property
+    def free_count(self) -> int:
+        n = _i64()
+        api.check(self._lib.pbz_pages_free_count(self._h, _c.byref(n)))
+        return n.value
+
+    def compact(self) -> np.ndarray:
+        """The page moves [n, 2] (from, to) that bring the pages in use to the front; tables already say so."""
+        pairs = np.empty((self.n_pages // 2 + 1, 2), dtype=np.int32)
+        n = _i64()
+        api.check(self._lib.pbz_pages_compact(self._h, pairs.ctypes.data, pairs.shape[0], _c.byref(n)))
+        return pairs[:n.value].copy()
+
+
+class PagedCache:
+    """Pools of compressed keys and values, {N, F} each, with the pages' owners.
+
+    head_dim 32, 64, 128 or 256; page_size a power of two from 16 to 1024; work_type: of N ("f32", "f16", "bf16").
+    pools: (k_N, k_F, v_N, v_F) that the program already holds, of `pool_shapes`; otherwise they are allocated here.
+    """
+
+    def __init__(self, head_dim: int, heads: int, n_pages: int, page_size: int = 64, work_type: str = "f32",
+                 transform: str = "dct", pools: Optional[Sequence] = None, device="cuda"):
+        self._lib = _library()
+        self.codec = api.Codec((int(head_dim),), work_type, "i8", transform=transform)
+        self.head_dim, self.heads, self.n_pages, self.page_size = int(head_dim), int(heads), int(n_pages), int(page_size)
+        self._struct = _Cache(n_pages=self.n_pages, heads=self.heads, page_size=self.page_size)
+        self._ref = _c.byref(self._struct)
+        self._h = self.codec._h
+        api.check(self._lib.pbz_cache_layout(self._h, self._ref, None, None))
+        self.pages = Pages(self.n_pages, self.page_size)
+        torch = api._torch()
+        if pools is None:
+            pools = [torch.zeros(shape, dtype=dtype, device=device) for shape, dtype in self.pool_shapes]
+        for pool, (shape, dtype) in zip(pools, self.pool_shapes):
+            if pool.dtype != dtype or tuple(pool.shape) != shape:
+                raise ValueError(f"a pool has to be {dtype} of shape {shape}, not {pool.dtype} of {tuple(pool.shape)}")
+        self.pools = self.k_N, self.k_F, self.v_N, self.v_F = tuple(pools)
+        for name, pool in zip(("k_N", "k_F", "v_N", "v_F"), self.pools):
+            setattr(self._struct, name, api._ptr(pool))
+        self.device = self.k_N.device
+        self._spaces = {}            # stream -> workspace
+        self._need = {}              # sizes of an attention call -> bytes of its workspace
+
+    @property
+    def pool_shapes(self):
+        torch = api._torch()
+        lines = (self.n_pages, self.heads, self.page_size)
+        n_type = api._torch_ftype(self.codec.work_type)
+        return [(lines, n_type), (lines + (self.head_dim,), torch.int8)] * 2
+
+    # ---- calls on tensors ------------------------------------------------------------------
+    def _lines(self, x, tokens: Optional[int], heads: int, name: str):
+        if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != self.head_dim or (tokens is not None and x.shape[0] != tokens):
+            raise ValueError(f"{name} has to be [tokens, {heads}, {self.head_dim}], not {tuple(x.shape)}")
+        if x.device != self.device:
+            raise ValueError(f"{name} is not on the cache's device")
+        token, head, element = x.stride()
+        if element != 1:
+            raise ValueError(f"{name}'s last dimension has to be contiguous")
+        return token, head
+
+    def _indices(self, t, dtype, shape, name: str) -> int:
+        if t.dtype != dtype or tuple(t.shape) != shape or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{name} has to be a contiguous {dtype} tensor of shape {shape} on the cache's device")
+        return t.data_ptr()
+
+    def append(self, k, v, slots) -> None:
+        """pbz_cache_append: compress keys and values [tokens, heads, head_dim] into their slots (int64, device;
+        page * page_size + place, -1 leaves a token out)."""
+        torch = api._torch()
+        tokens = k.shape[0]
+        if k.dtype != v.dtype or k.dtype not in api._FTYPE_OF:
+            raise ValueError("keys and values have to be of one float type")
+        k_strides, v_strides = self._lines(k, None, self.heads, "k"), self._lines(v, tokens, self.heads, "v")
+        at = self._indices(slots, torch.int64, (tokens,), "slots")
+        if tokens == 0:
+            return
+        api.check(self._lib.pbz_cache_append(self._h, self._ref, tokens, _Lines(k.data_ptr(), *k_strides),
+                                             _Lines(v.data_ptr(), *v_strides), api._ftype_of(k), at, api._stream()))
+
+    def copy_pages(self, pairs) -> None:
+        """pbz_cache_copy_pages: pairs [n, 2] (from, to), on the host."""
+        pairs = np.ascontiguousarray(pairs, dtype=np.int32).reshape(-1, 2)
+        if len(pairs):
+            api.check(self._lib.pbz_cache_copy_pages(self._h, self._ref, len(pairs), pairs.ctypes.data, api._stream()))
+
+    def attend(self, q, table, lengths, starts=None, max_new: Optional[int] = None, max_length: int = 0,
+               causal: bool = True, window: int = 0, scale: Optional[float] = None, out=None, lse=None, workspace=None):
+        """pbz_cache_attend: q [tokens, query heads, head_dim] (bfloat16 or float16) over the cache -> out, alike.
+
+        table [sequences, pages] and lengths [sequences], int32; starts [sequences + 1] int32, the rows of each
+        sequence's new tokens (None: one token a sequence).  max_new, max_length: the host's bounds of the runs of new
+        tokens and of the lengths, by which the work is dealt out (defaults: all tokens; the table's width).
+        lse: float32 [tokens, query heads], written.  scale: 1 / sqrt(head_dim) when None."""
+        torch = api._torch()
+        if q.dim() != 3:
+            raise ValueError("q has to be [tokens, query heads, head_dim]")
+        tokens, q_heads = q.shape[0], q.shape[1]
+        seqs = lengths.shape[0]
+        args = _Attention()
+        args.q_token_stride, args.q_head_stride = self._lines(q, None, q_heads, "q")
+        if table.dim() != 2 or table.dtype != torch.int32 or table.shape[0] != seqs or table.device != self.device or \
+                (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError(f"table has to be an int32 tensor [{seqs}, pages] with contiguous rows on the cache's device")
+        if out is None:
+            out = torch.empty((tokens, q_heads, self.head_dim), dtype=q.dtype, device=q.device)
+        elif out.dtype != q.dtype:
+            raise ValueError("out has to be of q's type")
+        args.out_token_stride, args.out_head_stride = self._lines(out, tokens, q_heads, "out")
+        args.lengths = self._indices(lengths, torch.int32, (seqs,), "lengths")
+        if starts is not None:
+            args.starts = self._indices(starts, torch.int32, (seqs + 1,), "starts")
+        if lse is not None:
+            args.lse = self._indices(lse, torch.float32, (tokens, q_heads), "lse")
+        if tokens == 0:
+            return out
+        args.q, args.out, args.table = q.data_ptr(), out.data_ptr(), table.data_ptr()
+        args.type, args.q_heads = api._FTYPE_OF.get(q.dtype, -1), q_heads
+        args.n_tokens, args.n_seqs = tokens, seqs
+        args.table_stride, args.max_pages = max(table.stride(0), table.shape[1]), table.shape[1]
+        args.max_new = tokens if max_new is None else int(max_new)
+        args.max_length, args.causal, args.window = int(max_length), 1 if causal else 0, int(window)
+        args.scale = 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale)
+        stream = api._stream()
+        if workspace is None:
+            sizes = (tokens, q_heads, seqs, args.max_pages, args.max_new, args.max_length, args.window, starts is None, args.type)
+            need = self._need.get(sizes)
+            if need is None:
+                need = self.workspace_bytes(args)
+                if len(self._need) < 256:
+                    self._need[sizes] = need
+            workspace = self._spaces.get(stream)
+            if workspace is None or workspace.numel() < need:
+                workspace = self._spaces[stream] = torch.empty(need, dtype=torch.uint8, device=self.device)
+        api.check(self._lib.pbz_cache_attend(self._h, self._ref, _c.byref(args), api._ptr(workspace),
+                                             workspace.numel() * workspace.element_size(), stream))
+        return out
+
+    def workspace_bytes(self, args: _Attention) -> int:
+        need = _c.c_size_t()
+        api.check(self._lib.pbz_cache_attend_workspace(self._h, self._ref, _c.byref(args), _c.byref(need)))
+        return need.value
+
+    # ---- sequences -------------------------------------------------------------------------
+    def open(self) -> int:
+        """A new, empty sequence."""
+        return self.pages.open()
+
+    def fork(self, sequence: int) -> int:
+        """A sequence that shares all of `sequence`'s pages; whichever is written first gets a copy of the last one."""
+        return self.pages.fork(sequence)
+
+    def close(self, sequence: int) -> None:
+        """Let a sequence's pages go."""
+        self.pages.close(sequence)
+
+    def truncate(self, sequence: int, length: int) -> None:
+        self.pages.truncate(sequence, length)
+
+    def length(self, sequence: int) -> int:
+        return self.pages.length(sequence)
+
+    def compact(self) -> int:
+        """Bring the pages in use to the front of the pools; returns how many were moved."""
+        pairs = self.pages.compact()
+        self.copy_pages(pairs)
+        return len(pairs)
+
+    def extend_and_append(self, sequences: Sequence[int], counts: Sequence[int], k, v) -> None:
+        """Append the next counts[b] tokens of each sequence; their rows follow one another in k and v."""
+        torch = api._torch()
+        if len(sequences) != len(counts) or sum(counts) != k.shape[0]:
+            raise ValueError("counts have to name every row of k, sequence by sequence")
+        if len(set(sequences)) != len(sequences):
+            raise ValueError("a sequence is named twice")
+        slots: List[np.ndarray] = []
+        before = [(seq, self.pages.length(seq)) for seq in sequences]
+        try:
+            for seq, count in zip(sequences, counts):
+                if count == 0:
+                    continue
+                found, copy = self.pages.extend(seq, count)
+                if copy:
+                    self.copy_pages([copy])      # at once: the page copied to may be copied from by the next
+                slots.append(found)
+        except api.PbzError:                     # too few pages: the sequences stay as long as they were
+            for seq, length in before:
+                self.pages.truncate(seq, length)
+            raise
+        if slots:
+            self.append(k, v, torch.from_numpy(np.concatenate(slots)).to(self.device))
+
+    def tables(self, sequences: Sequence[int]):
+        """(table, lengths) of the sequences, on the device, for `attend`."""
+        torch = api._torch()
+        lengths = [self.pages.length(s) for s in sequences]
+        width = max(1, max(-(-n // self.page_size) for n in lengths))
+        table = np.stack([self.pages.table(s, width) for s in sequences])
+        return torch.from_numpy(table).to(self.device), torch.tensor(lengths, dtype=torch.int32).to(self.device)
+
+    def attend_sequences(self, sequences: Sequence[int], counts: Sequence[int], q, **options):
+        """Attention of the last counts[b] tokens of each sequence (appended before); rows as in extend_and_append."""
+        torch = api._torch()
+        if len(sequences) != len(counts) or sum(counts) != q.shape[0]:
+            raise ValueError("counts have to name every row of q, sequence by sequence")
+        table, lengths = self.tables(sequences)
+        starts = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).to(self.device)
+        return self.attend(q, table, lengths, starts=starts, max_new=max(1, max(counts)), **options)

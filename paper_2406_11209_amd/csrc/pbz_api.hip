@@ -619,6 +619,10 @@ const char* pbz_status_string(int status) {
     case PBZ_ERR_STATE: return "too late in the handle's life for this call";
     case PBZ_ERR_CAPACITY:
       return "input beyond the capacity of the library's fixed scratch array (at most 4096 segments and 2^40 elements)";
+    case PBZ_ERR_ALIGNMENT: return "the cache's pools must be 16-byte aligned";
+    case PBZ_ERR_PAGES: return "a page outside the pool or written twice, or no free page left";
+    case PBZ_ERR_SEQUENCE: return "no such sequence";
+    case PBZ_ERR_MASK: return "a cache's codec must keep every index";
     default: return "unknown status";
   }
 }

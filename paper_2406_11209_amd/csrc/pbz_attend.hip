@@ -1,0 +1,383 @@
+// Attention over a paged compressed cache: the pass over keys and values (pbz_cache.h has the definition, pbz_cache.hip what
+// comes before and after).
+//
+// A wave takes 16 R query rows of one head of the cache and a run of positions, 16 positions to a matrix tile.
+//   scores   S^T = K q^T on the integer matrix cores: K's indices go from memory to the operand as they are, 16 bytes a lane; a row
+//            of q is 16-bit fixed point in two bytes, two products, 256 times the first plus the second, exact.  N and the row's
+//            scale are applied to the sum, so a key costs no conversion.
+//   softmax  with the running maximum and sum of its row.  A lane has 4 positions of one row per tile, so the maximum over
+//            positions is across four lanes; it is only taken when some score passes the old maximum by 8 (a weight by 2^8),
+//            which the wave votes on, so the usual tile exchanges nothing.  The sums stay per lane to the end.
+//   values   O^T += V^T P^T in FP16 with FP32 sums: the weights, times N over the largest N so far (a power of two) and 2^7, are in
+//            the registers where the product wants them (the order of positions within a product is free, as long as both operands
+//            have the same); the largest is 2^15, and what is 2^-29 of it is still a normal FP16 number.  V's bytes become FP16 integers
+//            by permutes: 0x6400 | (F + 128) is 1024 + 128 + F, minus 1152.
+// Lanes 16 apart share a position's line: a line of 128 is one 128-byte read of 8 (keys) or 16 lanes (values).
+#include "pbz_cache_internal.h"
+#include "pbz_device.h"
+
+namespace pbz {
+namespace {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kSlack = 8.f;          // by how much (in log2) a score may pass the maximum that the weights refer to
+
+// N of four neighbouring positions
+__device__ __forceinline__ f32x4 load_scales(const void* N, int type, int64_t i) {
+  if (type == PBZ_F32) return *reinterpret_cast<const f32x4*>(static_cast<const float*>(N) + i);
+  const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(N) + i);
+  f32x4 r;
+  if (type == PBZ_BF16) {
+    r[0] = __uint_as_float(u.x << 16);
+    r[1] = __uint_as_float(u.x & 0xffff0000u);
+    r[2] = __uint_as_float(u.y << 16);
+    r[3] = __uint_as_float(u.y & 0xffff0000u);
+  } else {
+    const f16x2 a = __builtin_bit_cast(f16x2, u.x), b = __builtin_bit_cast(f16x2, u.y);
+    r[0] = float(a[0]);
+    r[1] = float(a[1]);
+    r[2] = float(b[0]);
+    r[3] = float(b[1]);
+  }
+  return r;
+}
+
+// the bytes of one position's values that a lane holds: D / 16 neighbouring coefficients
+template <int D>
+__device__ __forceinline__ void load_values(const int8_t* p, uint32_t (&w)[D >= 64 ? D / 64 : 1]) {
+  if constexpr (D == 32) {
+    w[0] = *reinterpret_cast<const uint16_t*>(p);
+  } else if constexpr (D == 64) {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else if constexpr (D == 128) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    w[0] = u.x;
+    w[1] = u.y;
+  } else {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    w[0] = u.x;
+    w[1] = u.y;
+    w[2] = u.z;
+    w[3] = u.w;
+  }
+}
+
+// bytes kPair and kPair + 1 (both biased by 128) as FP16 integers
+template <int kPair>
+__device__ __forceinline__ uint32_t two_values(uint32_t bytes) {
+  const uint32_t biased = __builtin_amdgcn_perm(bytes, 0x64646464u, kPair == 0 ? 0x00050004u : 0x00070006u);
+  const f16x2 v = __builtin_bit_cast(f16x2, biased) - f16x2{_Float16(1152), _Float16(1152)};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// a workgroup's place in the order of the work: neighbours in that order share keys, and go to one die
+__device__ __forceinline__ uint32_t work_index(uint32_t blocks) {
+  const uint32_t per_die = (blocks + 7) / 8;
+  return (blockIdx.x % 8) * per_die + blockIdx.x / 8;
+}
+
+template <int D, int R, bool kFine>
+__global__ __launch_bounds__(256, R == 1 ? 2 : 2) void k_attend(const AttendCall a) {
+  constexpr int T = R == 1 ? 64 : 32;            // positions to a step
+  constexpr int U = T / 16;
+  constexpr int KS = D >= 64 ? D / 64 : 1;       // integer products to a line
+  constexpr int DT = D / 16;                     // value tiles
+  constexpr int VW = D >= 64 ? D / 64 : 1;       // 32-bit words of values a lane has of a position
+  const uint32_t work = work_index(a.blocks);
+  if (work >= a.blocks) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, quarter = lane >> 4;
+  const uint32_t row_block = a.row_blocks - 1 - work % a.row_blocks;      // the longest rows of a causal prompt first
+  const uint32_t split_block = work / a.row_blocks % a.split_blocks;
+  const uint32_t head_of_all = work / a.row_blocks / a.split_blocks;
+  const int head = int(head_of_all % uint32_t(a.cache.heads));
+  const int64_t seq = head_of_all / uint32_t(a.cache.heads);
+  const int split = int(split_block) * (4 / a.waves_rows) + wave / a.waves_rows;
+  if (split >= a.n_splits) return;
+
+  // the sequence's rows and positions, cut to what the arrays have
+  int64_t first = seq, last = seq + 1;
+  if (a.starts) {
+    first = a.starts[seq];
+    last = a.starts[seq + 1];
+    first = first < 0 ? 0 : first;
+    last = last > a.n_tokens ? a.n_tokens : last;
+  }
+  int64_t length = a.lengths[seq];
+  length = length < 0 ? 0 : length > a.table_tokens ? a.table_tokens : length;
+  const int64_t fresh = last > first ? last - first : 0;
+  const uint32_t rows = uint32_t(fresh) * uint32_t(a.groups);       // (fewer than 2^31 rows of q altogether)
+  const int32_t* table = a.table + seq * a.table_stride;
+  const uint32_t tiles_apart = a.row_blocks * uint32_t(a.waves_rows);
+  const int page_mask = a.cache.page_size - 1;
+
+  for (uint32_t tile = row_block * uint32_t(a.waves_rows) + wave % a.waves_rows; tile * (16 * R) < rows; tile += tiles_apart) {
+    // this lane's rows: where they are, what they see
+    int64_t place[R];                     // [token][query head]; -1: none
+    int low[R], high[R];
+    i32x4 q_high[R][KS], q_low[R][KS];
+    float q_scale[R];
+    const int64_t before = length - fresh;
+    const uint32_t groups = uint32_t(a.groups);
+    const uint32_t first_token = tile * (16 * R) / groups;                                // tokens of the tile
+    const uint32_t last_token = ((rows - tile * (16 * R) > 16 * R ? tile * (16 * R) + 16 * R : rows) - 1) / groups;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const uint32_t row = tile * (16 * R) + r * 16 + c;
+      const bool there = row < rows;
+      const uint32_t token = there ? row / groups : last_token;
+      const uint32_t g = there ? row - token * groups : 0;
+      const int64_t at = (first + token) * a.q_heads + int64_t(head) * a.groups + g;
+      place[r] = there ? at : -1;
+      const int64_t position = before + int64_t(token);
+      high[r] = int(a.causal ? position : length - 1);
+      const int64_t lowest = a.window > 0 ? position - a.window + 1 : 0;
+      low[r] = int(lowest < 0 ? 0 : lowest);
+      if (!there) high[r] = -1;
+      q_scale[r] = a.space.q_scale[at];
+      const int8_t* q = a.space.q + at * (2 * D);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const int offset = D == 32 ? (quarter & 1) * 16 : s * 64 + quarter * 16;
+        q_high[r][s] = *reinterpret_cast<const i32x4*>(q + offset);
+        q_low[r][s] = *reinterpret_cast<const i32x4*>(q + D + offset);
+        if (D == 32 && quarter >= 2) q_high[r][s] = q_low[r][s] = i32x4{0, 0, 0, 0};     // half of the product is not used
+      }
+    }
+    // positions that any row of the tile sees, and those that all of them see
+    const int64_t sees_from = a.window > 0 && before + int64_t(first_token) - a.window + 1 > 0 ? before + int64_t(first_token) - a.window + 1 : 0;
+    int64_t sees_to = a.causal ? before + int64_t(last_token) + 1 : length;
+    sees_to = sees_to < length ? sees_to : length;
+    const int64_t all_from = a.window > 0 ? before + int64_t(last_token) - a.window + 1 : 0;
+    int64_t all_to = a.causal ? before + int64_t(first_token) + 1 : length;
+    all_to = all_to < length ? all_to : length;
+    int64_t begin = (sees_from & ~int64_t(63)) + split * a.chunk;
+    int64_t end = split == a.n_splits - 1 ? sees_to : begin + a.chunk;
+    end = end < sees_to ? end : sees_to;
+
+    float top[R], total[R];
+    f32x4 sum[R][DT];
+    float widest = 0.f, narrow = 0.f;      // the largest N of the values so far (rounded up to a power of two); 2^7 over it
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      top[r] = kNegInf;
+      total[r] = 0.f;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) sum[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    for (int64_t at = begin; at < end; at += T) {
+      // lines of the 16 positions of each tile; a page outside the pool hides its positions
+      int64_t line[U];
+      bool whole = at >= all_from && at + T <= all_to;
+      int seen[U];                         // positions of the tile that there are
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t j = at + 16 * u;
+        int page = -1;
+        if (j < end) page = __builtin_amdgcn_readfirstlane(table[j >> a.cache.page_shift]);
+        const bool valid = page >= 0 && page < a.cache.n_pages;
+        seen[u] = valid ? int(length - j < 16 ? length - j : 16) : 0;
+        whole = whole && valid;
+        line[u] = (int64_t(valid ? page : 0) * a.cache.heads + head) * a.cache.page_size + (valid ? int(j) & page_mask : 0);
+      }
+      i32x4 key[U][KS];
+      f32x4 key_N[U], value_N[U];
+      uint32_t value[U][4][VW];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        key_N[u] = load_scales(a.cache.k_N, a.cache.n_type, line[u] + quarter * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) key_N[u][i] = fmaf(key_N[u][i], 0.f, key_N[u][i]);      // an infinity is a NaN: no score is -infinity but a hidden one's
+        const int8_t* k = a.cache.k_F + (line[u] + c) * D + (D == 32 ? (quarter & 1) * 16 : quarter * 16);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) key[u][s] = *reinterpret_cast<const i32x4*>(k + s * 64);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        value_N[u] = load_scales(a.cache.v_N, a.cache.n_type, line[u] + quarter * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_values<D>(a.cache.v_F + (line[u] + quarter * 4 + i) * D + c * (D / 16), value[u][i]);
+      }
+
+      // scores, in units of ln 2
+      float x[R][U][4];
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          i32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+          for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(key[u][s], q_high[r][s], acc, 0, 0, 0);
+          acc = acc << 8;
+#pragma unroll
+          for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(key[u][s], q_low[r][s], acc, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[r][u][i] = float(acc[i]) * (key_N[u][i] * q_scale[r]);
+        }
+      if (!whole) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int j = int(at) + 16 * u + quarter * 4 + i;
+            const bool there = quarter * 4 + i < seen[u];
+            if (!there) value_N[u][i] = 0.f;
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+              if (!there || j > high[r] || j < low[r]) x[r][u][i] = kNegInf;
+          }
+      }
+
+      // have the references to grow?
+      float wide = 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) wide = fmaxf(wide, fabsf(value_N[u][i]) < __builtin_huge_valf() ? fabsf(value_N[u][i]) : 0.f);
+      float most[R];
+      bool grow = wide > widest;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        most[r] = x[r][0][0];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) most[r] = fmaxf(most[r], x[r][u][i]);
+        grow = grow || most[r] > top[r] + kSlack;
+      }
+      if (__any(grow)) {
+        for (int apart = 1; apart < 64; apart <<= 1) wide = fmaxf(wide, __shfl_xor(wide, apart));
+        float wider = widest;
+        if (wide > widest) {
+          // the next power of two, within the range whose reciprocal is a normal number
+          const uint32_t up = (__float_as_uint(wide) + 0x7fffffu) & 0x7f800000u;
+          wider = __uint_as_float(up > 0x7e000000u ? 0x7e000000u : up < 0x04000000u ? 0x04000000u : up);
+        }
+        const float narrower = wider > 0.f ? 128.f / wider : 0.f;
+        const float shrink = wider > 0.f ? widest / wider : 1.f;
+        widest = wider;
+        narrow = narrower;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          float m = fmaxf(top[r], most[r]);
+          m = fmaxf(m, __shfl_xor(m, 16));
+          m = fmaxf(m, __shfl_xor(m, 32));
+          const float factor = m == kNegInf ? 1.f : __builtin_amdgcn_exp2f(top[r] - m);
+          top[r] = m;
+          total[r] *= factor;
+#pragma unroll
+          for (int t = 0; t < DT; ++t) sum[r][t] *= factor * shrink;
+        }
+      }
+
+      // weights
+      f16x8 p[R][T / 32], p_low[R][T / 32];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const f32x4 n = value_N[u] * narrow;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const float reference = top[r] == kNegInf ? 0.f : top[r];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float e = __builtin_amdgcn_exp2f(x[r][u][i] - reference);
+            total[r] += e;
+            float w = e * n[i];
+            if (!whole && x[r][u][i] == kNegInf) w = 0.f;      // N may be anything there
+            const _Float16 h = _Float16(w);
+            p[r][u / 2][(u % 2) * 4 + i] = h;
+            if constexpr (kFine) p_low[r][u / 2][(u % 2) * 4 + i] = _Float16(w - float(h));
+          }
+        }
+      }
+
+      // values
+#pragma unroll
+      for (int b = 0; b < T / 32; ++b)
+#pragma unroll
+        for (int h = 0; h < VW; ++h) {
+          u32x4 tiles[4];                  // of coefficients 4 h .. 4 h + 3: 8 positions each
+#pragma unroll
+          for (int pair = 0; pair < 4; ++pair) {
+            const uint32_t w0 = value[2 * b + pair / 2][(2 * pair) % 4][h] ^ 0x80808080u;
+            const uint32_t w1 = value[2 * b + pair / 2][(2 * pair) % 4 + 1][h] ^ 0x80808080u;
+            const uint32_t lo = __builtin_amdgcn_perm(w1, w0, 0x05010400u), hi = __builtin_amdgcn_perm(w1, w0, 0x07030602u);
+            tiles[0][pair] = two_values<0>(lo);
+            tiles[1][pair] = two_values<1>(lo);
+            tiles[2][pair] = two_values<0>(hi);
+            tiles[3][pair] = two_values<1>(hi);
+          }
+#pragma unroll
+          for (int t = 0; t < (D == 32 ? 2 : 4); ++t) {
+            const f16x8 v = __builtin_bit_cast(f16x8, tiles[t]);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              sum[r][4 * h + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[r][b], sum[r][4 * h + t], 0, 0, 0);
+              if constexpr (kFine)
+                sum[r][4 * h + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p_low[r][b], sum[r][4 * h + t], 0, 0, 0);
+            }
+          }
+        }
+    }
+
+    // a lane has coefficients (4 quarter + i) DT + t of its rows
+    const float unit = widest * (1.f / (128.f * 127.f));
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float l = total[r];
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      if (place[r] < 0) continue;
+      if (l != l) top[r] = 0.f;            // a row that sees a NaN is one, also where it sees nothing else
+      const int64_t to = int64_t(split) * a.n_tokens * a.q_heads + place[r];
+      if (quarter == 0) a.space.state[to] = make_float2(top[r], l);
+      if (top[r] == kNegInf) continue;
+      float* out = a.space.sums + to * D + quarter * 4 * DT;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (DT >= 4) {
+#pragma unroll
+          for (int t = 0; t < DT; t += 4) {
+            const f32x4 v = {sum[r][t][i], sum[r][t + 1][i], sum[r][t + 2][i], sum[r][t + 3][i]};
+            *reinterpret_cast<f32x4*>(out + i * DT + t) = v * unit;
+          }
+        } else {
+          *reinterpret_cast<float2*>(out + i * DT) = make_float2(sum[r][0][i] * unit, sum[r][1][i] * unit);
+        }
+      }
+    }
+  }
+}
+
+template <int D>
+int launch(int rows, bool fine, const AttendCall& call, hipStream_t s) {
+  const dim3 grid(unsigned((call.blocks + 7) / 8 * 8)), block(256);
+  if (rows == 16) {
+    if (fine) k_attend<D, 1, true><<<grid, block, 0, s>>>(call);
+    else k_attend<D, 1, false><<<grid, block, 0, s>>>(call);
+  } else {
+    if (fine) k_attend<D, 2, true><<<grid, block, 0, s>>>(call);
+    else k_attend<D, 2, false><<<grid, block, 0, s>>>(call);
+  }
+  return hip_status(hipGetLastError());
+}
+
+}  // namespace
+
+int launch_attend(int dim, int rows, bool fine, const AttendCall& call, hipStream_t s) {
+  switch (dim) {
+    case 32: return launch<32>(rows, fine, call, s);
+    case 64: return launch<64>(rows, fine, call, s);
+    case 128: return launch<128>(rows, fine, call, s);
+    default: return launch<256>(rows, fine, call, s);
+  }
+}
+
+}  // namespace pbz

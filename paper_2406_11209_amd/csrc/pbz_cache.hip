@@ -1,0 +1,643 @@
+// The paged compressed cache (pbz_cache.h): checks and launches, the kernels that append lines and copy pages, and what an
+// attention call does before and after its pass over keys and values (pbz_attend.hip).
+#include <algorithm>
+#include <cmath>
+#include <vector>
+
+#include "pbz_cache_internal.h"
+#include "pbz_device.h"
+#include "pbz_line_transform.h"
+
+namespace pbz {
+namespace {
+
+constexpr int kMaxSplits = 256;
+constexpr int64_t kComputeWaves = 2048;      // waves that keep the chip busy: two to a SIMD
+constexpr int kPairsPerLaunch = 256;
+
+// 32 neighbouring elements as T; `wide`: the address is a multiple of 16 bytes
+template <typename T>
+__device__ __forceinline__ void load_run(const void* p, int type, int64_t at, bool wide, T (&v)[32]) {
+  if (type == PBZ_F64) {
+    const double* x = static_cast<const double*>(p) + at;
+    if (wide) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 2) {
+        const double2 u = *reinterpret_cast<const double2*>(x + i);
+        v[i] = T(u.x);
+        v[i + 1] = T(u.y);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = T(x[i]);
+    }
+  } else if (type == PBZ_F32) {
+    const float* x = static_cast<const float*>(p) + at;
+    if (wide) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 4) {
+        const float4 u = *reinterpret_cast<const float4*>(x + i);
+        v[i] = T(u.x);
+        v[i + 1] = T(u.y);
+        v[i + 2] = T(u.z);
+        v[i + 3] = T(u.w);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = T(x[i]);
+    }
+  } else {
+    const uint16_t* x = static_cast<const uint16_t*>(p) + at;
+    uint32_t w[16];
+    if (wide) {
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const uint4 u = *reinterpret_cast<const uint4*>(x + 2 * i);
+        w[i] = u.x;
+        w[i + 1] = u.y;
+        w[i + 2] = u.z;
+        w[i + 3] = u.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] = uint32_t(x[2 * i]) | (uint32_t(x[2 * i + 1]) << 16);
+    }
+    if (type == PBZ_BF16) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        v[2 * i] = T(__uint_as_float(w[i] << 16));
+        v[2 * i + 1] = T(__uint_as_float(w[i] & 0xffff0000u));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        v[2 * i] = T(float(__builtin_bit_cast(_Float16, uint16_t(w[i]))));
+        v[2 * i + 1] = T(float(__builtin_bit_cast(_Float16, uint16_t(w[i] >> 16))));
+      }
+    }
+  }
+}
+
+// the largest magnitude of a line, and whether all of its values are finite: the same in its L lanes
+template <typename T, int L>
+__device__ __forceinline__ T line_max(const T (&v)[32]) {
+  T most = T(0);
+#pragma unroll
+  for (int i = 0; i < 32; ++i) most = fmax(most, fabs(v[i]));
+#pragma unroll
+  for (int apart = 1; apart < L; apart <<= 1) most = fmax(most, __shfl_xor(most, apart));
+  return most;
+}
+template <typename T, int L>
+__device__ __forceinline__ bool line_finite(const T (&v)[32]) {
+  int bad = 0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) bad |= !(fabs(v[i]) < T(__builtin_huge_valf()));
+#pragma unroll
+  for (int apart = 1; apart < L; apart <<= 1) bad |= __shfl_xor(bad, apart);
+  return !bad;
+}
+
+// ---- append ----------------------------------------------------------------------------------------------------------
+
+struct AppendCall {
+  CacheGeom cache;
+  pbz_lines x[2];          // keys, values
+  const int64_t* slots;
+  int64_t lines;           // tokens * 2 * heads
+  int32_t type;
+  int32_t wide;
+};
+
+// L = D / 32 lanes to a line; a wave's indices go through LDS, where a lane's coefficients, L apart, become 32 neighbouring bytes.
+template <int kTf, int D>
+__global__ __launch_bounds__(256) void k_append(const AppendCall a) {
+  constexpr int L = D / 32, kLines = 64 / L, kPitch = D + 4;      // the pitch keeps lines L apart off one bank
+  __shared__ uint32_t staged[4][kLines * kPitch / 4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane % L, in_wave = lane / L;
+  const int64_t asked = (int64_t(blockIdx.x) * 4 + wave) * kLines + in_wave;
+  const bool there = asked < a.lines;
+  const int64_t line = there ? asked : a.lines - 1;
+  const uint32_t heads = uint32_t(a.cache.heads);
+  const int64_t pair = line / heads;                              // [token][keys, values]
+  const int head = int(line - pair * heads);
+  const int64_t token = pair >> 1;
+  const bool values = pair & 1;
+  const pbz_lines& x = a.x[values];
+  double v[32];
+  load_run(x.data, a.type, token * x.token_stride + head * x.head_stride + part * 32, a.wide != 0, v);
+  const int64_t slot = a.slots[token];
+  const bool finite = line_finite<double, L>(v);
+  line::forward<kTf, double, L>(v, part);
+  const double N = line_max<double, L>(v);
+  uint8_t* bytes = reinterpret_cast<uint8_t*>(staged[wave]) + in_wave * kPitch;
+#pragma unroll
+  for (int k = 0; k < 32; ++k) {
+    const int index = N > 0.0 && finite ? int(rint(127.0 * v[k] / N)) : 0;
+    bytes[line::coefficient<kTf, L>(part, k)] = uint8_t(index);
+  }
+  wave_lds_sync();
+  const int64_t page = slot >> a.cache.page_shift;
+  if (!there || slot < 0 || page >= a.cache.n_pages) return;
+  const int64_t to = (page * heads + head) * a.cache.page_size + (slot & (a.cache.page_size - 1));
+  const uint32_t* from = staged[wave] + (in_wave * kPitch + part * 32) / 4;
+  uint4* F = reinterpret_cast<uint4*>(const_cast<int8_t*>(values ? a.cache.v_F : a.cache.k_F) + to * D + part * 32);
+  F[0] = make_uint4(from[0], from[1], from[2], from[3]);
+  F[1] = make_uint4(from[4], from[5], from[6], from[7]);
+  if (part == 0)
+    store_float(const_cast<void*>(values ? a.cache.v_N : a.cache.k_N), a.cache.n_type, to, finite ? N : __builtin_nan(""));
+}
+
+// ---- copies of pages ---------------------------------------------------------------------------------------------------
+
+struct CopyCall {
+  void* pool[4];
+  int64_t page_bytes[4];       // multiples of 16
+  int64_t page_total;
+  int32_t pairs[2 * kPairsPerLaunch];
+};
+
+// a workgroup has 16 KiB of a page's four parts, laid end to end
+__global__ __launch_bounds__(256) void k_copy_pages(const CopyCall a) {
+  const int64_t from = a.pairs[2 * blockIdx.y], to = a.pairs[2 * blockIdx.y + 1];
+  uint4 held[4];
+  char* where[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    int64_t at = (int64_t(blockIdx.x) * 1024 + i * 256 + threadIdx.x) * 16;
+    char* pool = nullptr;
+    int64_t size = 0;
+    if (at < a.page_total) {
+#pragma unroll
+      for (int part = 0; part < 4; ++part) {
+        if (!pool && at < a.page_bytes[part]) {
+          pool = static_cast<char*>(a.pool[part]) + at;
+          size = a.page_bytes[part];
+        }
+        at -= a.page_bytes[part];
+      }
+    }
+    where[i] = pool ? pool + to * size : nullptr;
+    if (pool) held[i] = *reinterpret_cast<const uint4*>(pool + from * size);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (where[i]) *reinterpret_cast<uint4*>(where[i]) = held[i];
+}
+
+// ---- attention: queries before, results after ----------------------------------------------------------------------------
+
+struct QueryCall {
+  const void* q;
+  int64_t token_stride, head_stride;
+  int64_t rows;            // tokens * query heads
+  int32_t q_heads;
+  int32_t type;
+  int32_t wide;
+  float scale;             // scale log2(e) / 127
+  AttendSpace space;
+};
+
+// Transformed, and held relative to the row's largest coefficient in 16 bits, +-32639 = 127 * 256 + 127, high and low byte signed.
+template <int kTf, int D>
+__global__ __launch_bounds__(256) void k_queries(const QueryCall a) {
+  constexpr int L = D / 32, kLines = 64 / L, kPitch = 2 * D + 4;
+  __shared__ uint32_t staged[4][kLines * kPitch / 4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane % L, in_wave = lane / L;
+  const int64_t asked = (int64_t(blockIdx.x) * 4 + wave) * kLines + in_wave;
+  const bool there = asked < a.rows;
+  const int64_t row = there ? asked : a.rows - 1;
+  const int64_t token = row / a.q_heads;
+  float v[32];
+  load_run(a.q, a.type, token * a.token_stride + (row - token * a.q_heads) * a.head_stride + part * 32, a.wide != 0, v);
+  const bool finite = line_finite<float, L>(v);
+  line::forward<kTf, float, L>(v, part);
+  const float most = line_max<float, L>(v);
+  const float up = finite && most > 0.f ? 32639.f / most : 0.f;
+  const float sign = a.scale < 0.f ? -1.f : 1.f;
+  uint8_t* bytes = reinterpret_cast<uint8_t*>(staged[wave]) + in_wave * kPitch;
+#pragma unroll
+  for (int k = 0; k < 32; ++k) {
+    const int index = up < __builtin_huge_valf() ? int(rintf(fminf(fmaxf(v[k] * up, -32639.f), 32639.f) * sign)) : 0;
+    const int high = (index + 128) >> 8;
+    const int at = line::coefficient<kTf, L>(part, k);
+    bytes[at] = uint8_t(high);
+    bytes[D + at] = uint8_t(index - 256 * high);
+  }
+  wave_lds_sync();
+  if (!there) return;
+  const uint32_t* from = staged[wave] + (in_wave * kPitch + part * 64) / 4;
+  uint4* q = reinterpret_cast<uint4*>(a.space.q + row * (2 * D) + part * 64);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i] = make_uint4(from[4 * i], from[4 * i + 1], from[4 * i + 2], from[4 * i + 3]);
+  if (part == 0) a.space.q_scale[row] = finite ? most * (1.f / 32639.f) * fabsf(a.scale) : __builtin_nanf("");
+}
+
+struct FinishCall {
+  AttendSpace space;
+  void* out;
+  float* lse;
+  int64_t token_stride, head_stride;
+  int64_t rows;
+  const int32_t* starts;
+  int64_t n_seqs;
+  int32_t q_heads;
+  int32_t type;
+  int32_t wide;
+  int32_t n_splits;
+};
+
+// Joins the splits of a row, divides by the sum and transforms back.  kRows rows to a workgroup: 256 / L where there is one split, else
+// one, whose splits the threads share.
+template <int kTf, int D, bool kJoin>
+__global__ __launch_bounds__(256) void k_finish(const FinishCall a) {
+  constexpr int L = D / 32, kRows = kJoin ? 1 : 256 / L, kColumns = D / 4, kPitch = D + 4;
+  constexpr int kGroups = kJoin ? 256 / kColumns : 1;
+  __shared__ float staged[kRows * kGroups * kPitch];
+  __shared__ float weight[kMaxSplits];
+  __shared__ float joined[8];
+  const int64_t first = int64_t(blockIdx.x) * kRows;
+  const int tid = threadIdx.x;
+  if constexpr (kJoin) {
+    const int64_t row = first;
+    float2 state = make_float2(-__builtin_huge_valf(), 0.f);
+    if (tid < a.n_splits) state = a.space.state[int64_t(tid) * a.rows + row];
+    float most = state.x;
+    for (int apart = 1; apart < 64; apart <<= 1) most = fmaxf(most, __shfl_xor(most, apart));
+    if ((tid & 63) == 0) joined[tid >> 6] = most;
+    __syncthreads();
+    most = fmaxf(fmaxf(joined[0], joined[1]), fmaxf(joined[2], joined[3]));
+    const float w = state.x == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(state.x - most);
+    weight[tid] = state.x == -__builtin_huge_valf() ? -1.f : w;
+    float total = state.x == -__builtin_huge_valf() ? 0.f : w * state.y;
+    for (int apart = 1; apart < 64; apart <<= 1) total += __shfl_xor(total, apart);
+    if ((tid & 63) == 0) joined[4 + (tid >> 6)] = total;
+    __syncthreads();
+    total = (joined[4] + joined[5]) + (joined[6] + joined[7]);
+    const int column = tid % kColumns, group = tid / kColumns;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = group; s < a.n_splits; s += kGroups) {
+      const float f = weight[s];
+      if (f < 0.f) continue;
+      const float4 u = *reinterpret_cast<const float4*>(a.space.sums + (int64_t(s) * a.rows + row) * D + column * 4);
+      sum.x += f * u.x;
+      sum.y += f * u.y;
+      sum.z += f * u.z;
+      sum.w += f * u.w;
+    }
+    const float by = most == -__builtin_huge_valf() ? 0.f : 1.f / total;
+    float* to = staged + group * kPitch + column * 4;
+    to[0] = sum.x * by;
+    to[1] = sum.y * by;
+    to[2] = sum.z * by;
+    to[3] = sum.w * by;
+    __syncthreads();
+    if (tid < D) {
+      float s = 0.f;
+      for (int g = 0; g < kGroups; ++g) s += staged[g * kPitch + tid];
+      staged[tid] = s;                       // this thread's own column: nobody else reads it before the barrier
+    }
+    if (tid == 0 && a.lse) a.lse[row] = (most + __builtin_amdgcn_logf(total)) * 0.693147180559945309f;
+    __syncthreads();
+  } else {
+    for (int item = tid; item < kRows * kColumns; item += 256) {
+      const int64_t row = first + item / kColumns;
+      float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (row < a.rows) {
+        const float2 state = a.space.state[row];
+        if (state.x != -__builtin_huge_valf()) {
+          const float by = 1.f / state.y;
+          u = *reinterpret_cast<const float4*>(a.space.sums + row * D + (item % kColumns) * 4);
+          u = make_float4(u.x * by, u.y * by, u.z * by, u.w * by);
+        }
+        if (item % kColumns == 0 && a.lse) a.lse[row] = (state.x + __builtin_amdgcn_logf(state.y)) * 0.693147180559945309f;
+      }
+      *reinterpret_cast<float4*>(staged + (item / kColumns) * kPitch + (item % kColumns) * 4) = u;
+    }
+    __syncthreads();
+  }
+  if (tid >= kRows * L) return;              // whole lines: L divides
+  const int part = tid % L, in_block = tid / L;
+  const int64_t row = first + in_block;
+  const int64_t token = row / a.q_heads;
+  const int64_t head = row - token * a.q_heads;
+  float v[32];
+#pragma unroll
+  for (int k = 0; k < 32; ++k) v[k] = staged[in_block * kPitch + line::coefficient<kTf, L>(part, k)];
+  line::inverse<kTf, float, L>(v, part);
+  if (row >= a.rows) return;
+  if (a.starts && (token < a.starts[0] || token >= a.starts[a.n_seqs])) {      // a row of no sequence
+#pragma unroll
+    for (int k = 0; k < 32; ++k) v[k] = 0.f;
+    if (part == 0 && a.lse) a.lse[row] = -__builtin_huge_valf();
+  }
+  uint16_t* out = static_cast<uint16_t*>(a.out) + token * a.token_stride + head * a.head_stride + part * 32;
+  uint32_t w[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    uint16_t x, y;
+    if (a.type == PBZ_BF16) {
+      x = float_to_bf16_bits(v[2 * k]);
+      y = float_to_bf16_bits(v[2 * k + 1]);
+    } else {
+      x = __builtin_bit_cast(uint16_t, _Float16(v[2 * k]));
+      y = __builtin_bit_cast(uint16_t, _Float16(v[2 * k + 1]));
+    }
+    w[k] = uint32_t(x) | (uint32_t(y) << 16);
+  }
+  if (a.wide) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(out)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      out[2 * k] = uint16_t(w[k]);
+      out[2 * k + 1] = uint16_t(w[k] >> 16);
+    }
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+// f(transform, D) with both as types
+template <typename F>
+void for_line(int transform, int dim, F&& f) {
+  const auto sized = [&](auto tf) {
+    if (dim == 32) f(tf, std::integral_constant<int, 32>());
+    else if (dim == 64) f(tf, std::integral_constant<int, 64>());
+    else if (dim == 128) f(tf, std::integral_constant<int, 128>());
+    else f(tf, std::integral_constant<int, 256>());
+  };
+  if (transform == PBZ_TRANSFORM_HAAR) sized(std::integral_constant<int, kTfHaar>());
+  else sized(std::integral_constant<int, kTfDct>());
+}
+
+bool aligned(const void* p, uintptr_t to = 16) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+int check_geometry(const pbz_codec* c, const pbz_cache* cache) {
+  if (!c || !cache) return PBZ_ERR_NULL;
+  if (c->ndim != 1 || (c->vol != 32 && c->vol != 64 && c->vol != 128 && c->vol != 256)) return PBZ_ERR_BLOCK_SHAPE;
+  if (c->itype != PBZ_I8 || c->ftype == PBZ_F64) return PBZ_ERR_TYPE;
+  if (c->kept != c->vol) return PBZ_ERR_MASK;
+  const int64_t size = cache->page_size;
+  if (size < 16 || size > 1024 || (size & (size - 1)) || cache->heads < 1 || cache->heads > 65535 || cache->n_pages < 1 ||
+      cache->n_pages > INT32_MAX || cache->n_pages > (int64_t(1) << 40) / (int64_t(cache->heads) * size * c->vol))
+    return PBZ_ERR_SHAPE;
+  return PBZ_OK;
+}
+
+int check_cache(const pbz_codec* c, const pbz_cache* cache, CacheGeom* g) {
+  const int st = check_geometry(c, cache);
+  if (st != PBZ_OK) return st;
+  if (!cache->k_N || !cache->k_F || !cache->v_N || !cache->v_F) return PBZ_ERR_NULL;
+  if (!aligned(cache->k_N) || !aligned(cache->k_F) || !aligned(cache->v_N) || !aligned(cache->v_F)) return PBZ_ERR_ALIGNMENT;
+  g->n_pages = cache->n_pages;
+  g->heads = cache->heads;
+  g->page_size = cache->page_size;
+  g->page_shift = __builtin_ctz(unsigned(cache->page_size));
+  g->n_type = c->ftype;
+  g->k_N = cache->k_N;
+  g->k_F = static_cast<const int8_t*>(cache->k_F);
+  g->v_N = cache->v_N;
+  g->v_F = static_cast<const int8_t*>(cache->v_F);
+  return PBZ_OK;
+}
+
+constexpr int64_t kMaxElements = int64_t(1) << 40;
+
+bool stride_ok(int64_t stride, int64_t count) { return stride >= 0 && (count < 2 || stride <= kMaxElements / (count - 1)); }
+
+// how an attention call is dealt out; every field follows from sizes that the host has
+struct AttendPlan {
+  int64_t rows;            // of q
+  int tile;                // query rows to a wave
+  int waves_rows;
+  int64_t row_blocks, split_blocks;
+  int64_t n_splits, chunk;
+  size_t q_bytes, scale_bytes, state_bytes, sum_bytes;
+  size_t total() const { return q_bytes + scale_bytes + state_bytes + sum_bytes; }
+};
+
+size_t padded(uint64_t n) { return size_t((n + 255) / 256 * 256); }
+
+int plan_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_attention* a, AttendPlan* p) {
+  const int st = check_geometry(c, cache);
+  if (st != PBZ_OK) return st;
+  if (!a) return PBZ_ERR_NULL;
+  if (a->type != PBZ_BF16 && a->type != PBZ_F16) return PBZ_ERR_TYPE;
+  if (a->q_heads < 1 || a->q_heads % cache->heads || a->n_tokens < 1 || a->n_seqs < 1 || a->n_seqs > INT32_MAX ||
+      a->max_pages < 1 || a->max_pages > INT32_MAX / cache->page_size || a->table_stride < a->max_pages ||
+      a->table_stride > kMaxElements / a->n_seqs || a->max_new < 1 || a->max_length < 0 || a->window < 0 ||
+      a->window > INT32_MAX || a->n_tokens > INT32_MAX / a->q_heads || (!a->starts && a->n_tokens != a->n_seqs))
+    return PBZ_ERR_SHAPE;
+  if (!std::isfinite(a->scale)) return PBZ_ERR_SCALAR;
+  const int groups = a->q_heads / cache->heads;
+  const int64_t fresh = a->starts ? std::min(a->max_new, a->n_tokens) : 1;
+  const int64_t rows = fresh * groups;
+  p->rows = a->n_tokens * a->q_heads;
+  p->tile = rows <= 16 ? 16 : 32;
+  const int64_t tiles = (rows + p->tile - 1) / p->tile;
+  int64_t length = a->max_pages * cache->page_size;
+  if (a->max_length > 0) length = std::min(length, a->max_length);
+  if (a->window > 0) length = std::min(length, a->window + fresh + 63);
+  // splits of the positions, where rows alone do not fill the chip; a split shorter than 128 would not pay for its record
+  const int64_t alone = a->n_seqs * cache->heads * tiles;
+  int64_t splits = alone >= kComputeWaves ? 1 : (kComputeWaves + alone - 1) / alone;
+  splits = std::max<int64_t>(1, std::min<int64_t>({splits, kMaxSplits, length / 128}));
+  p->chunk = ((length + splits - 1) / splits + 63) / 64 * 64;
+  p->n_splits = (length + p->chunk - 1) / p->chunk;
+  p->waves_rows = p->n_splits == 1 || tiles >= 4 ? 4 : tiles >= 2 ? 2 : 1;
+  const int waves_splits = 4 / p->waves_rows;
+  p->row_blocks = (tiles + p->waves_rows - 1) / p->waves_rows;
+  p->split_blocks = (p->n_splits + waves_splits - 1) / waves_splits;
+  if (p->row_blocks > INT32_MAX / (a->n_seqs * cache->heads) / p->split_blocks) return PBZ_ERR_SHAPE;
+  p->q_bytes = padded(uint64_t(p->rows) * 2 * c->vol);
+  p->scale_bytes = padded(uint64_t(p->rows) * sizeof(float));
+  p->state_bytes = padded(uint64_t(p->rows) * p->n_splits * sizeof(float2));
+  p->sum_bytes = padded(uint64_t(p->rows) * p->n_splits * c->vol * sizeof(float));
+  return PBZ_OK;
+}
+
+}  // namespace
+}  // namespace pbz
+
+using namespace pbz;
+
+extern "C" {
+
+int pbz_cache_layout(const pbz_codec* c, const pbz_cache* cache, size_t* n_bytes, size_t* f_bytes) {
+  const int st = check_geometry(c, cache);
+  if (st != PBZ_OK) return st;
+  const size_t lines = size_t(cache->n_pages) * size_t(cache->heads) * size_t(cache->page_size);
+  if (n_bytes) *n_bytes = lines * size_t(ftype_bytes(c->ftype));
+  if (f_bytes) *f_bytes = lines * size_t(c->vol);
+  return PBZ_OK;
+}
+
+int pbz_cache_append(const pbz_codec* c, const pbz_cache* cache, int64_t n_tokens, const pbz_lines* k, const pbz_lines* v,
+                     pbz_ftype type, const int64_t* slots, void* stream) {
+  AppendCall call;
+  const int st = check_cache(c, cache, &call.cache);
+  if (st != PBZ_OK) return st;
+  if (!k || !v || !k->data || !v->data || !slots) return PBZ_ERR_NULL;
+  if (type != PBZ_F64 && type != PBZ_F32 && type != PBZ_BF16 && type != PBZ_F16) return PBZ_ERR_TYPE;
+  const int bytes = ftype_bytes(type);
+  call.wide = 1;
+  int i = 0;
+  for (const pbz_lines* x : {k, v}) {
+    if (n_tokens < 1 || n_tokens > INT32_MAX / cache->heads || !stride_ok(x->token_stride, n_tokens) ||
+        !stride_ok(x->head_stride, cache->heads))
+      return PBZ_ERR_SHAPE;
+    if (!aligned(x->data) || x->token_stride * bytes % 16 || x->head_stride * bytes % 16) call.wide = 0;
+    call.x[i++] = *x;
+  }
+  call.slots = slots;
+  call.lines = n_tokens * 2 * cache->heads;
+  call.type = type;
+  c->used.store(true);
+  const int64_t lines = 256 / (c->vol / 32);
+  const dim3 grid(unsigned((call.lines + lines - 1) / lines));
+  for_line(c->transform, c->vol, [&](auto tf, auto dim) {
+    k_append<decltype(tf)::value, decltype(dim)::value><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(call);
+  });
+  return hip_status(hipGetLastError());
+}
+
+int pbz_cache_copy_pages(const pbz_codec* c, const pbz_cache* cache, int64_t n_pairs, const int32_t* pairs, void* stream) {
+  CacheGeom g;
+  const int st = check_cache(c, cache, &g);
+  if (st != PBZ_OK) return st;
+  if (!pairs) return PBZ_ERR_NULL;
+  if (n_pairs < 1 || n_pairs > cache->n_pages) return PBZ_ERR_SHAPE;
+  // every page in the pool, written at most once, and not read as well
+  for (int64_t i = 0; i < 2 * n_pairs; ++i)
+    if (pairs[i] < 0 || pairs[i] >= cache->n_pages) return PBZ_ERR_PAGES;
+  if (n_pairs <= 32) {
+    for (int64_t i = 0; i < n_pairs; ++i)
+      for (int64_t j = 0; j < n_pairs; ++j)
+        if (pairs[2 * i + 1] == pairs[2 * j] || (i != j && pairs[2 * i + 1] == pairs[2 * j + 1])) return PBZ_ERR_PAGES;
+  } else {
+    try {
+      std::vector<uint8_t> role(size_t(cache->n_pages), 0);      // 1 read, 2 written
+      for (int64_t i = 0; i < n_pairs; ++i) role[size_t(pairs[2 * i])] = 1;
+      for (int64_t i = 0; i < n_pairs; ++i) {
+        uint8_t& to = role[size_t(pairs[2 * i + 1])];
+        if (to) return PBZ_ERR_PAGES;
+        to = 2;
+      }
+    } catch (...) {
+      return PBZ_ERR_ALLOC;
+    }
+  }
+  CopyCall call;
+  const int64_t lines = int64_t(cache->heads) * cache->page_size;
+  void* const pools[4] = {cache->k_F, cache->v_F, cache->k_N, cache->v_N};
+  call.page_total = 0;
+  for (int i = 0; i < 4; ++i) {
+    call.pool[i] = pools[i];
+    call.page_bytes[i] = lines * (i < 2 ? c->vol : ftype_bytes(c->ftype));
+    call.page_total += call.page_bytes[i];
+  }
+  const unsigned parts = unsigned((call.page_total + 16383) / 16384);
+  for (int64_t at = 0; at < n_pairs; at += kPairsPerLaunch) {
+    const int64_t n = std::min<int64_t>(kPairsPerLaunch, n_pairs - at);
+    std::copy(pairs + 2 * at, pairs + 2 * (at + n), call.pairs);
+    k_copy_pages<<<dim3(parts, unsigned(n)), 256, 0, static_cast<hipStream_t>(stream)>>>(call);
+    const int launched = hip_status(hipGetLastError());
+    if (launched != PBZ_OK) return launched;
+  }
+  return PBZ_OK;
+}
+
+int pbz_cache_attend_workspace(const pbz_codec* c, const pbz_cache* cache, const pbz_attention* a, size_t* bytes) {
+  if (!bytes) return PBZ_ERR_NULL;
+  AttendPlan p;
+  const int st = plan_attend(c, cache, a, &p);
+  if (st != PBZ_OK) return st;
+  *bytes = p.total();
+  return PBZ_OK;
+}
+
+int pbz_cache_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_attention* a, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  AttendCall call;
+  int st = check_cache(c, cache, &call.cache);
+  if (st != PBZ_OK) return st;
+  AttendPlan p;
+  st = plan_attend(c, cache, a, &p);
+  if (st != PBZ_OK) return st;
+  if (!a->q || !a->out || !a->lengths || !a->table || !workspace) return PBZ_ERR_NULL;
+  for (int64_t stride : {a->q_token_stride, a->out_token_stride})
+    if (!stride_ok(stride, a->n_tokens)) return PBZ_ERR_SHAPE;
+  for (int64_t stride : {a->q_head_stride, a->out_head_stride})
+    if (!stride_ok(stride, a->q_heads)) return PBZ_ERR_SHAPE;
+  if (workspace_bytes < p.total() || !aligned(workspace)) return PBZ_ERR_WORKSPACE;
+  char* at = static_cast<char*>(workspace);
+  AttendSpace& space = call.space;
+  space.q = reinterpret_cast<int8_t*>(at);
+  space.q_scale = reinterpret_cast<float*>(at += p.q_bytes);
+  space.state = reinterpret_cast<float2*>(at += p.scale_bytes);
+  space.sums = reinterpret_cast<float*>(at += p.state_bytes);
+  c->used.store(true);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const int L = c->vol / 32;
+
+  QueryCall query;
+  query.q = a->q;
+  query.token_stride = a->q_token_stride;
+  query.head_stride = a->q_head_stride;
+  query.rows = p.rows;
+  query.q_heads = a->q_heads;
+  query.type = a->type;
+  query.wide = aligned(a->q) && a->q_token_stride % 8 == 0 && a->q_head_stride % 8 == 0;
+  query.scale = a->scale * float(1.4426950408889634074 / 127.0);
+  query.space = space;
+  const dim3 query_grid(unsigned((p.rows + 256 / L - 1) / (256 / L)));
+  for_line(c->transform, c->vol, [&](auto tf, auto dim) {
+    k_queries<decltype(tf)::value, decltype(dim)::value><<<query_grid, 256, 0, s>>>(query);
+  });
+  st = hip_status(hipGetLastError());
+  if (st != PBZ_OK) return st;
+
+  call.starts = a->starts;
+  call.lengths = a->lengths;
+  call.table = a->table;
+  call.table_stride = a->table_stride;
+  call.n_tokens = a->n_tokens;
+  call.n_seqs = a->n_seqs;
+  call.table_tokens = a->max_pages * cache->page_size;
+  call.window = a->window;
+  call.chunk = p.chunk;
+  call.causal = a->causal != 0;
+  call.q_heads = a->q_heads;
+  call.groups = a->q_heads / cache->heads;
+  call.n_splits = int32_t(p.n_splits);
+  call.waves_rows = p.waves_rows;
+  call.row_blocks = uint32_t(p.row_blocks);
+  call.split_blocks = uint32_t(p.split_blocks);
+  call.blocks = uint32_t(p.row_blocks * p.split_blocks * a->n_seqs * cache->heads);
+  st = launch_attend(c->vol, p.tile, a->type == PBZ_F16, call, s);
+  if (st != PBZ_OK) return st;
+
+  FinishCall finish;
+  finish.space = space;
+  finish.out = a->out;
+  finish.lse = a->lse;
+  finish.token_stride = a->out_token_stride;
+  finish.head_stride = a->out_head_stride;
+  finish.rows = p.rows;
+  finish.starts = a->starts;
+  finish.n_seqs = a->n_seqs;
+  finish.q_heads = a->q_heads;
+  finish.type = a->type;
+  finish.wide = aligned(a->out) && a->out_token_stride % 8 == 0 && a->out_head_stride % 8 == 0;
+  finish.n_splits = int32_t(p.n_splits);
+  for_line(c->transform, c->vol, [&](auto tf, auto dim) {
+    constexpr int kTf = decltype(tf)::value, D = decltype(dim)::value;
+    if (p.n_splits > 1) k_finish<kTf, D, true><<<dim3(unsigned(p.rows)), 256, 0, s>>>(finish);
+    else k_finish<kTf, D, false><<<dim3(unsigned((p.rows + 256 / L - 1) / (256 / L))), 256, 0, s>>>(finish);
+  });
+  return hip_status(hipGetLastError());
+}
+
+}  // extern "C"
