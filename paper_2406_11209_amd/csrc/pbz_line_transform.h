@@ -39,7 +39,7 @@ template <int n> struct Previous { static constexpr int control = n == 4 ? 0xB1 
 
 // 1 / (2 cos(pi (2m+1) / (2n))) for m < n / 2, n = 64, 128, 256 one after the other
 template <typename T>
-struct Secants {
+struct alignas(32) Secants {
   T v[32 + 64 + 128];
   constexpr Secants() : v() {
     int at = 0;
@@ -68,23 +68,38 @@ struct Path {
   }
 };
 
+// the 32 factors of a lane at the split of n lanes (1 where it has the sums), read all at once
+template <typename T, int n>
+__device__ __forceinline__ void factors(T (&f)[32], int half, int place) {
+  typedef T Four __attribute__((ext_vector_type(4)));
+  const Four* table = reinterpret_cast<const Four*>(secants(T()) + (n == 2 ? 0 : n == 4 ? 32 : 96) + 32 * place);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const Four u = table[i];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[4 * i + j] = half ? u[j] : T(1);
+  }
+}
+
 template <typename T, int n>       // n lanes
 __device__ __forceinline__ void split(T (&v)[32], int half, int place) {
-  const T* f = secants(T()) + (n == 2 ? 0 : n == 4 ? 32 : 96) + 32 * place;
+  T f[32];
+  factors<T, n>(f, half, place);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int j = 31 - i;
     const T ti = moved<Mirror<n>::control>(v[i]), tj = moved<Mirror<n>::control>(v[j]);
     const T si = v[i] + tj, sj = v[j] + ti, di = ti - v[j], dj = tj - v[i];
-    v[i] = half ? di * f[i] : si;
-    v[j] = half ? dj * f[j] : sj;
+    v[i] = (half ? di : si) * f[i];
+    v[j] = (half ? dj : sj) * f[j];
   }
 }
 template <typename T, int n>
 __device__ __forceinline__ void unsplit(T (&v)[32], int half, int place) {
-  const T* f = secants(T()) + (n == 2 ? 0 : n == 4 ? 32 : 96) + 32 * place;
+  T f[32];
+  factors<T, n>(f, half, place);
 #pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = half ? v[i] * f[i] : v[i];
+  for (int i = 0; i < 32; ++i) v[i] *= f[i];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int j = 31 - i;
