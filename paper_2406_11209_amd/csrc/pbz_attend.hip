@@ -28,24 +28,20 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kSlack = 8.f;          // by how much (in log2) a score may pass the maximum that the weights refer to
 
-// N of four neighbouring positions
-__device__ __forceinline__ f32x4 load_scales(const void* N, int type, int64_t i) {
-  if (type == PBZ_F32) return *reinterpret_cast<const f32x4*>(static_cast<const float*>(N) + i);
-  const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(N) + i);
-  f32x4 r;
-  if (type == PBZ_BF16) {
-    r[0] = __uint_as_float(u.x << 16);
-    r[1] = __uint_as_float(u.x & 0xffff0000u);
-    r[2] = __uint_as_float(u.y << 16);
-    r[3] = __uint_as_float(u.y & 0xffff0000u);
+// N of four neighbouring positions, as stored
+template <int kN> struct Scales { using Raw = uint2; };
+template <> struct Scales<PBZ_F32> { using Raw = f32x4; };
+template <int kN>
+__device__ __forceinline__ f32x4 scales(typename Scales<kN>::Raw u) {
+  if constexpr (kN == PBZ_F32) {
+    return u;
+  } else if constexpr (kN == PBZ_BF16) {
+    return f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                 __uint_as_float(u.y & 0xffff0000u)};
   } else {
     const f16x2 a = __builtin_bit_cast(f16x2, u.x), b = __builtin_bit_cast(f16x2, u.y);
-    r[0] = float(a[0]);
-    r[1] = float(a[1]);
-    r[2] = float(b[0]);
-    r[3] = float(b[1]);
+    return f32x4{float(a[0]), float(a[1]), float(b[0]), float(b[1])};
   }
-  return r;
 }
 
 // the bytes of one position's values that a lane holds: D / 16 neighbouring coefficients
@@ -82,9 +78,9 @@ __device__ __forceinline__ uint32_t work_index(uint32_t blocks) {
   return (blockIdx.x % 8) * per_die + blockIdx.x / 8;
 }
 
-template <int D, int R, bool kFine>
-__global__ __launch_bounds__(256, R == 1 ? 2 : 2) void k_attend(const AttendCall a) {
-  constexpr int T = R == 1 ? 64 : 32;            // positions to a step
+template <int D, int R, bool kFine, int kN>
+__global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) void k_attend(const AttendCall a) {
+  constexpr int T = 32;            // positions to a step
   constexpr int U = T / 16;
   constexpr int KS = D >= 64 ? D / 64 : 1;       // integer products to a line
   constexpr int DT = D / 16;                     // value tiles
@@ -113,9 +109,14 @@ __global__ __launch_bounds__(256, R == 1 ? 2 : 2) void k_attend(const AttendCall
   length = length < 0 ? 0 : length > a.table_tokens ? a.table_tokens : length;
   const int64_t fresh = last > first ? last - first : 0;
   const uint32_t rows = uint32_t(fresh) * uint32_t(a.groups);       // (fewer than 2^31 rows of q altogether)
-  const int32_t* table = a.table + seq * a.table_stride;
+  // (the constant address space: uniform reads through the scalar cache)
+  const auto* table = (const __attribute__((address_space(4))) int32_t*)(a.table + seq * a.table_stride);
   const uint32_t tiles_apart = a.row_blocks * uint32_t(a.waves_rows);
   const int page_mask = a.cache.page_size - 1;
+  using Raw = typename Scales<kN>::Raw;
+  constexpr int kNBytes = kN == PBZ_F32 ? 4 : 2;
+  const uint32_t key_offset = c * D + (D == 32 ? (quarter & 1) * 16 : quarter * 16);      // a lane's place within 16 lines
+  const uint32_t value_offset = quarter * 4 * D + c * (D / 16), scale_offset = quarter * 4 * kNBytes;
 
   for (uint32_t tile = row_block * uint32_t(a.waves_rows) + wave % a.waves_rows; tile * (16 * R) < rows; tile += tiles_apart) {
     // this lane's rows: where they are, what they see
@@ -141,6 +142,7 @@ __global__ __launch_bounds__(256, R == 1 ? 2 : 2) void k_attend(const AttendCall
       low[r] = int(lowest < 0 ? 0 : lowest);
       if (!there) high[r] = -1;
       q_scale[r] = a.space.q_scale[at];
+      if (q_scale[r] == 0.f) q_scale[r] = 0x1p-100f;       // all of the row's products are zero; a hidden one stays -infinity
       const int8_t* q = a.space.q + at * (2 * D);
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
@@ -161,57 +163,71 @@ __global__ __launch_bounds__(256, R == 1 ? 2 : 2) void k_attend(const AttendCall
     int64_t end = split == a.n_splits - 1 ? sees_to : begin + a.chunk;
     end = end < sees_to ? end : sees_to;
 
-    float top[R], total[R];
+    float top[R], reference[R], total[R];
     f32x4 sum[R][DT];
     float widest = 0.f, narrow = 0.f;      // the largest N of the values so far (rounded up to a power of two); 2^7 over it
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       top[r] = kNegInf;
+      reference[r] = 0.f;
       total[r] = 0.f;
 #pragma unroll
       for (int t = 0; t < DT; ++t) sum[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    for (int64_t at = begin; at < end; at += T) {
-      // lines of the 16 positions of each tile; a page outside the pool hides its positions
-      int64_t line[U];
-      bool whole = at >= all_from && at + T <= all_to;
-      int seen[U];                         // positions of the tile that there are
+    // lines of the 16 positions of each tile of a step, and how many of them there are; a page outside the pool has none
+    const auto look_up = [&](int64_t at, int64_t (&line)[U], int (&there)[U]) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int64_t j = at + 16 * u;
-        int page = -1;
-        if (j < end) page = __builtin_amdgcn_readfirstlane(table[j >> a.cache.page_shift]);
+        const int page = j < end ? table[j >> a.cache.page_shift] : -1;
         const bool valid = page >= 0 && page < a.cache.n_pages;
-        seen[u] = valid ? int(length - j < 16 ? length - j : 16) : 0;
-        whole = whole && valid;
+        there[u] = valid ? int(length - j < 16 ? length - j : 16) : 0;
         line[u] = (int64_t(valid ? page : 0) * a.cache.heads + head) * a.cache.page_size + (valid ? int(j) & page_mask : 0);
       }
-      i32x4 key[U][KS];
-      f32x4 key_N[U], value_N[U];
+    };
+    const auto load_keys = [&](const int64_t (&line)[U], i32x4 (&key)[U][KS], Raw (&N)[U]) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int8_t* k = a.cache.k_F + line[u] * D;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) key[u][s] = *reinterpret_cast<const i32x4*>(k + (key_offset + s * 64));
+        N[u] = *reinterpret_cast<const Raw*>(static_cast<const char*>(a.cache.k_N) + line[u] * kNBytes + scale_offset);
+      }
+    };
+    // Keys are read a step ahead, into the registers that the products before them have left; values while the scores are taken.
+    int64_t line[U], next_line[U];
+    int there[U], next_there[U];
+    i32x4 key[U][KS];
+    Raw key_raw[U];
+    if (begin < end) {
+      look_up(begin, line, there);
+      load_keys(line, key, key_raw);
+    }
+    for (int64_t at = begin; at < end; at += T) {
+      bool whole = at >= all_from && at + T <= all_to;
+#pragma unroll
+      for (int u = 0; u < U; ++u) whole = whole && there[u] == 16;
+      look_up(at + T, next_line, next_there);
+      Raw value_raw[U];
       uint32_t value[U][4][VW];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        key_N[u] = load_scales(a.cache.k_N, a.cache.n_type, line[u] + quarter * 4);
+        const int8_t* v = a.cache.v_F + line[u] * D;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) key_N[u][i] = fmaf(key_N[u][i], 0.f, key_N[u][i]);      // an infinity is a NaN: no score is -infinity but a hidden one's
-        const int8_t* k = a.cache.k_F + (line[u] + c) * D + (D == 32 ? (quarter & 1) * 16 : quarter * 16);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) key[u][s] = *reinterpret_cast<const i32x4*>(k + s * 64);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        value_N[u] = load_scales(a.cache.v_N, a.cache.n_type, line[u] + quarter * 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) load_values<D>(a.cache.v_F + (line[u] + quarter * 4 + i) * D + c * (D / 16), value[u][i]);
+        for (int i = 0; i < 4; ++i) load_values<D>(v + (value_offset + i * D), value[u][i]);
+        value_raw[u] = *reinterpret_cast<const Raw*>(static_cast<const char*>(a.cache.v_N) + line[u] * kNBytes + scale_offset);
       }
 
-      // scores, in units of ln 2
+      // scores, over the row's scale, in units of ln 2
       float x[R][U][4];
 #pragma unroll
-      for (int r = 0; r < R; ++r)
+      for (int u = 0; u < U; ++u) {
+        f32x4 N = scales<kN>(key_raw[u]);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int i = 0; i < 4; ++i) N[i] = fmaf(N[i], 0.f, N[i]);      // an infinity is a NaN: no score is -infinity but a hidden one's
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
           i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
           for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(key[u][s], q_high[r][s], acc, 0, 0, 0);
@@ -219,20 +235,30 @@ __global__ __launch_bounds__(256, R == 1 ? 2 : 2) void k_attend(const AttendCall
 #pragma unroll
           for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(key[u][s], q_low[r][s], acc, 0, 0, 0);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[r][u][i] = float(acc[i]) * (key_N[u][i] * q_scale[r]);
+          for (int i = 0; i < 4; ++i) x[r][u][i] = float(acc[i]) * N[i];
         }
+      }
+      if (at + T < end) load_keys(next_line, key, key_raw);
+      f32x4 value_N[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) value_N[u] = scales<kN>(value_raw[u]);
       if (!whole) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int j = int(at) + 16 * u + quarter * 4 + i;
-            const bool there = quarter * 4 + i < seen[u];
-            if (!there) value_N[u][i] = 0.f;
+            const bool is = quarter * 4 + i < there[u];
+            if (!is) value_N[u][i] = 0.f;
 #pragma unroll
             for (int r = 0; r < R; ++r)
-              if (!there || j > high[r] || j < low[r]) x[r][u][i] = kNegInf;
+              if (!is || j > high[r] || j < low[r]) x[r][u][i] = kNegInf;
           }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        line[u] = next_line[u];
+        there[u] = next_there[u];
       }
 
       // have the references to grow?
@@ -240,7 +266,7 @@ __global__ __launch_bounds__(256, R == 1 ? 2 : 2) void k_attend(const AttendCall
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) wide = fmaxf(wide, fabsf(value_N[u][i]) < __builtin_huge_valf() ? fabsf(value_N[u][i]) : 0.f);
+        for (int i = 0; i < 4; ++i) wide = fmaxf(wide, fabsf(value_N[u][i]));
       float most[R];
       bool grow = wide > widest;
 #pragma unroll
@@ -250,9 +276,15 @@ __global__ __launch_bounds__(256, R == 1 ? 2 : 2) void k_attend(const AttendCall
         for (int u = 0; u < U; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) most[r] = fmaxf(most[r], x[r][u][i]);
+        most[r] *= q_scale[r];
         grow = grow || most[r] > top[r] + kSlack;
       }
       if (__any(grow)) {
+        wide = 0.f;                          // of what is finite
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) wide = fmaxf(wide, fabsf(value_N[u][i]) < __builtin_huge_valf() ? fabsf(value_N[u][i]) : 0.f);
         for (int apart = 1; apart < 64; apart <<= 1) wide = fmaxf(wide, __shfl_xor(wide, apart));
         float wider = widest;
         if (wide > widest) {
@@ -260,10 +292,9 @@ __global__ __launch_bounds__(256, R == 1 ? 2 : 2) void k_attend(const AttendCall
           const uint32_t up = (__float_as_uint(wide) + 0x7fffffu) & 0x7f800000u;
           wider = __uint_as_float(up > 0x7e000000u ? 0x7e000000u : up < 0x04000000u ? 0x04000000u : up);
         }
-        const float narrower = wider > 0.f ? 128.f / wider : 0.f;
         const float shrink = wider > 0.f ? widest / wider : 1.f;
         widest = wider;
-        narrow = narrower;
+        narrow = wider > 0.f ? 128.f / wider : 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
           float m = fmaxf(top[r], most[r]);
@@ -271,6 +302,7 @@ __global__ __launch_bounds__(256, R == 1 ? 2 : 2) void k_attend(const AttendCall
           m = fmaxf(m, __shfl_xor(m, 32));
           const float factor = m == kNegInf ? 1.f : __builtin_amdgcn_exp2f(top[r] - m);
           top[r] = m;
+          reference[r] = m == kNegInf ? 0.f : m;
           total[r] *= factor;
 #pragma unroll
           for (int t = 0; t < DT; ++t) sum[r][t] *= factor * shrink;
@@ -284,10 +316,9 @@ __global__ __launch_bounds__(256, R == 1 ? 2 : 2) void k_attend(const AttendCall
         const f32x4 n = value_N[u] * narrow;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          const float reference = top[r] == kNegInf ? 0.f : top[r];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float e = __builtin_amdgcn_exp2f(x[r][u][i] - reference);
+            const float e = __builtin_amdgcn_exp2f(fmaf(x[r][u][i], q_scale[r], -reference[r]));
             total[r] += e;
             float w = e * n[i];
             if (!whole && x[r][u][i] == kNegInf) w = 0.f;      // N may be anything there
@@ -356,17 +387,25 @@ __global__ __launch_bounds__(256, R == 1 ? 2 : 2) void k_attend(const AttendCall
   }
 }
 
-template <int D>
+template <int D, int kN>
 int launch(int rows, bool fine, const AttendCall& call, hipStream_t s) {
-  const dim3 grid(unsigned((call.blocks + 7) / 8 * 8)), block(256);
+  const dim3 grid((call.blocks + 7) / 8 * 8), block(256);
   if (rows == 16) {
-    if (fine) k_attend<D, 1, true><<<grid, block, 0, s>>>(call);
-    else k_attend<D, 1, false><<<grid, block, 0, s>>>(call);
+    if (fine) k_attend<D, 1, true, kN><<<grid, block, 0, s>>>(call);
+    else k_attend<D, 1, false, kN><<<grid, block, 0, s>>>(call);
   } else {
-    if (fine) k_attend<D, 2, true><<<grid, block, 0, s>>>(call);
-    else k_attend<D, 2, false><<<grid, block, 0, s>>>(call);
+    if (fine) k_attend<D, 2, true, kN><<<grid, block, 0, s>>>(call);
+    else k_attend<D, 2, false, kN><<<grid, block, 0, s>>>(call);
   }
   return hip_status(hipGetLastError());
+}
+template <int D>
+int launch(int rows, bool fine, const AttendCall& call, hipStream_t s) {
+  switch (call.cache.n_type) {
+    case PBZ_F32: return launch<D, PBZ_F32>(rows, fine, call, s);
+    case PBZ_BF16: return launch<D, PBZ_BF16>(rows, fine, call, s);
+    default: return launch<D, PBZ_F16>(rows, fine, call, s);
+  }
 }
 
 }  // namespace
