@@ -44,6 +44,12 @@ __device__ __forceinline__ f32x4 scales(typename Scales<kN>::Raw u) {
   }
 }
 
+template <int kN>
+__device__ __forceinline__ typename Scales<kN>::Raw load_N(const void* N, int64_t line, int quarter) {
+  constexpr int kBytes = kN == PBZ_F32 ? 4 : 2;
+  return *reinterpret_cast<const typename Scales<kN>::Raw*>(static_cast<const char*>(N) + line * kBytes + uint32_t(quarter * 4 * kBytes));
+}
+
 // the bytes of one position's values that a lane holds: D / 16 neighbouring coefficients
 template <int D>
 __device__ __forceinline__ void load_values(const int8_t* p, uint32_t (&w)[D >= 64 ? D / 64 : 1]) {
@@ -78,71 +84,115 @@ __device__ __forceinline__ uint32_t work_index(uint32_t blocks) {
   return (blockIdx.x % 8) * per_die + blockIdx.x / 8;
 }
 
-template <int D, int R, bool kFine, int kN>
-__global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) void k_attend(const AttendCall a) {
-  constexpr int T = 32;            // positions to a step
-  constexpr int U = T / 16;
-  constexpr int KS = D >= 64 ? D / 64 : 1;       // integer products to a line
-  constexpr int DT = D / 16;                     // value tiles
-  constexpr int VW = D >= 64 ? D / 64 : 1;       // 32-bit words of values a lane has of a position
-  const uint32_t work = work_index(a.blocks);
-  if (work >= a.blocks) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = lane & 15, quarter = lane >> 4;
-  const uint32_t row_block = a.row_blocks - 1 - work % a.row_blocks;      // the longest rows of a causal prompt first
-  const uint32_t split_block = work / a.row_blocks % a.split_blocks;
-  const uint32_t head_of_all = work / a.row_blocks / a.split_blocks;
-  const int head = int(head_of_all % uint32_t(a.cache.heads));
-  const int64_t seq = head_of_all / uint32_t(a.cache.heads);
-  const int split = int(split_block) * (4 / a.waves_rows) + wave / a.waves_rows;
-  if (split >= a.n_splits) return;
-
-  // the sequence's rows and positions, cut to what the arrays have
-  int64_t first = seq, last = seq + 1;
-  if (a.starts) {
-    first = a.starts[seq];
-    last = a.starts[seq + 1];
-    first = first < 0 ? 0 : first;
-    last = last > a.n_tokens ? a.n_tokens : last;
-  }
-  int64_t length = a.lengths[seq];
-  length = length < 0 ? 0 : length > a.table_tokens ? a.table_tokens : length;
-  const int64_t fresh = last > first ? last - first : 0;
-  const uint32_t rows = uint32_t(fresh) * uint32_t(a.groups);       // (fewer than 2^31 rows of q altogether)
+// What a workgroup works on: a sequence's rows and positions, cut to what the arrays have, and a head of the cache.
+struct Part {
+  int head, split;
+  uint32_t row_block;
+  int64_t first;           // first row of q
+  int fresh, length;       // new tokens, positions
+  uint32_t rows;           // query rows: new tokens times query heads of the head
   // (the constant address space: uniform reads through the scalar cache)
-  const auto* table = (const __attribute__((address_space(4))) int32_t*)(a.table + seq * a.table_stride);
-  const uint32_t tiles_apart = a.row_blocks * uint32_t(a.waves_rows);
-  const int page_mask = a.cache.page_size - 1;
-  using Raw = typename Scales<kN>::Raw;
-  constexpr int kNBytes = kN == PBZ_F32 ? 4 : 2;
-  const uint32_t key_offset = c * D + (D == 32 ? (quarter & 1) * 16 : quarter * 16);      // a lane's place within 16 lines
-  const uint32_t value_offset = quarter * 4 * D + c * (D / 16), scale_offset = quarter * 4 * kNBytes;
+  const __attribute__((address_space(4))) int32_t* table;
 
-  for (uint32_t tile = row_block * uint32_t(a.waves_rows) + wave % a.waves_rows; tile * (16 * R) < rows; tile += tiles_apart) {
-    // this lane's rows: where they are, what they see
-    int64_t place[R];                     // [token][query head]; -1: none
-    int low[R], high[R];
-    i32x4 q_high[R][KS], q_low[R][KS];
-    float q_scale[R];
-    const int64_t before = length - fresh;
+  __device__ __forceinline__ bool find(const AttendCall& a, int wave) {
+    const uint32_t work = work_index(a.blocks);
+    if (work >= a.blocks) return false;
+    row_block = a.row_blocks - 1 - work % a.row_blocks;      // the longest rows of a causal prompt first
+    const uint32_t split_block = work / a.row_blocks % a.split_blocks;
+    const uint32_t head_of_all = work / a.row_blocks / a.split_blocks;
+    head = int(head_of_all % uint32_t(a.cache.heads));
+    const int64_t seq = head_of_all / uint32_t(a.cache.heads);
+    split = int(split_block) * (4 / a.waves_rows) + wave / a.waves_rows;
+    if (split >= a.n_splits) return false;
+    int64_t last = seq + 1;
+    first = seq;
+    if (a.starts) {
+      first = a.starts[seq];
+      last = a.starts[seq + 1];
+      first = first < 0 ? 0 : first;
+      last = last > a.n_tokens ? a.n_tokens : last;
+    }
+    fresh = last > first ? int(last - first) : 0;
+    const int64_t asked = a.lengths[seq];
+    length = int(asked < 0 ? 0 : asked > a.table_tokens ? a.table_tokens : asked);
+    rows = uint32_t(fresh) * uint32_t(a.groups);             // (fewer than 2^31 rows of q altogether)
+    table = (const __attribute__((address_space(4))) int32_t*)(a.table + seq * a.table_stride);
+    return true;
+  }
+};
+
+// The positions that rows see: any of them from .. to, all of them all_from .. all_to (each cut to what there is).
+struct Range {
+  int from, to, all_from, all_to;
+  __device__ __forceinline__ Range(const AttendCall& a, const Part& part, uint32_t first_row, uint32_t rows) {
+    const int groups = a.groups, before = part.length - part.fresh;
+    const int first_at = before + int(first_row / groups), last_at = before + int((first_row + rows - 1) / groups);
+    const int window = int(a.window);
+    from = window > 0 && first_at - window + 1 > 0 ? first_at - window + 1 : 0;
+    to = a.causal && last_at + 1 < part.length ? last_at + 1 : part.length;
+    all_from = window > 0 ? last_at - window + 1 : 0;
+    all_to = a.causal && first_at + 1 < part.length ? first_at + 1 : part.length;
+  }
+};
+
+// The lines of 16 positions: the first one's index, and how many there are; a page outside the pool has none.
+struct Lines16 {
+  int64_t line;
+  int there;
+  __device__ __forceinline__ void find(const AttendCall& a, const Part& part, int at, int end) {
+    const int page = at < end ? part.table[at >> a.cache.page_shift] : -1;
+    const bool valid = page >= 0 && page < a.cache.n_pages;
+    there = valid ? (part.length - at < 16 ? part.length - at : 16) : 0;
+    line = (int64_t(valid ? page : 0) * a.cache.heads + part.head) * a.cache.page_size +
+           (valid ? at & (a.cache.page_size - 1) : 0);
+  }
+};
+
+// Keys of 16 positions as a lane holds them, and their N.
+template <int D, int kN>
+struct Keys {
+  static constexpr int KS = D >= 64 ? D / 64 : 1;       // integer products to a line
+  i32x4 F[KS];
+  typename Scales<kN>::Raw N;
+  __device__ __forceinline__ void load(const AttendCall& a, int64_t line, int c, int quarter) {
+    const int8_t* k = a.cache.k_F + line * D;
+    const uint32_t offset = c * D + (D == 32 ? (quarter & 1) * 16 : quarter * 16);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) F[s] = *reinterpret_cast<const i32x4*>(k + (offset + s * 64));
+    N = load_N<kN>(a.cache.k_N, line, quarter);
+  }
+};
+
+// A wave's 16 R rows of one head: what it keeps of them while positions go by, 32 to a step.
+template <int D, int R, bool kFine, int kN>
+struct Rows {
+  static constexpr int KS = Keys<D, kN>::KS;
+  static constexpr int DT = D / 16;                      // value tiles
+  int64_t place[R];                                      // [token][query head]; -1: none
+  int low[R], high[R];                                   // positions that a row sees
+  i32x4 q_high[R][KS], q_low[R][KS];
+  float q_scale[R];
+  float top[R], reference[R], total[R];
+  f32x4 sum[R][DT];
+  float widest, narrow;      // the largest N of the values so far (rounded up to a power of two); 2^7 over it
+  f16x8 p[R], p_low[R];      // weights of a step
+
+  __device__ __forceinline__ void begin(const AttendCall& a, const Part& part, uint32_t first_row, int c, int quarter) {
     const uint32_t groups = uint32_t(a.groups);
-    const uint32_t first_token = tile * (16 * R) / groups;                                // tokens of the tile
-    const uint32_t last_token = ((rows - tile * (16 * R) > 16 * R ? tile * (16 * R) + 16 * R : rows) - 1) / groups;
+    const int before = part.length - part.fresh;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const uint32_t row = tile * (16 * R) + r * 16 + c;
-      const bool there = row < rows;
-      const uint32_t token = there ? row / groups : last_token;
-      const uint32_t g = there ? row - token * groups : 0;
-      const int64_t at = (first + token) * a.q_heads + int64_t(head) * a.groups + g;
+      const uint32_t asked = first_row + r * 16 + c;
+      const bool there = asked < part.rows;
+      const uint32_t row = there ? asked : part.rows - 1;
+      const uint32_t token = row / groups;
+      const int64_t at = (part.first + token) * a.q_heads + int64_t(part.head) * a.groups + (row - token * groups);
       place[r] = there ? at : -1;
-      const int64_t position = before + int64_t(token);
-      high[r] = int(a.causal ? position : length - 1);
-      const int64_t lowest = a.window > 0 ? position - a.window + 1 : 0;
-      low[r] = int(lowest < 0 ? 0 : lowest);
-      if (!there) high[r] = -1;
+      const int position = before + int(token);
+      high[r] = !there ? -1 : a.causal ? position : part.length - 1;
+      low[r] = a.window > 0 && position - int(a.window) + 1 > 0 ? position - int(a.window) + 1 : 0;
       q_scale[r] = a.space.q_scale[at];
-      if (q_scale[r] == 0.f) q_scale[r] = 0x1p-100f;       // all of the row's products are zero; a hidden one stays -infinity
+      if (q_scale[r] == 0.f) q_scale[r] = 0x1p-100f;     // all of the row's products are zero; a hidden one stays -infinity
       const int8_t* q = a.space.q + at * (2 * D);
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
@@ -151,214 +201,138 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
         q_low[r][s] = *reinterpret_cast<const i32x4*>(q + D + offset);
         if (D == 32 && quarter >= 2) q_high[r][s] = q_low[r][s] = i32x4{0, 0, 0, 0};     // half of the product is not used
       }
-    }
-    // positions that any row of the tile sees, and those that all of them see
-    const int64_t sees_from = a.window > 0 && before + int64_t(first_token) - a.window + 1 > 0 ? before + int64_t(first_token) - a.window + 1 : 0;
-    int64_t sees_to = a.causal ? before + int64_t(last_token) + 1 : length;
-    sees_to = sees_to < length ? sees_to : length;
-    const int64_t all_from = a.window > 0 ? before + int64_t(last_token) - a.window + 1 : 0;
-    int64_t all_to = a.causal ? before + int64_t(first_token) + 1 : length;
-    all_to = all_to < length ? all_to : length;
-    int64_t begin = (sees_from & ~int64_t(63)) + split * a.chunk;
-    int64_t end = split == a.n_splits - 1 ? sees_to : begin + a.chunk;
-    end = end < sees_to ? end : sees_to;
-
-    float top[R], reference[R], total[R];
-    f32x4 sum[R][DT];
-    float widest = 0.f, narrow = 0.f;      // the largest N of the values so far (rounded up to a power of two); 2^7 over it
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
       top[r] = kNegInf;
       reference[r] = 0.f;
       total[r] = 0.f;
 #pragma unroll
       for (int t = 0; t < DT; ++t) sum[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    widest = narrow = 0.f;
+  }
 
-    // lines of the 16 positions of each tile of a step, and how many of them there are; a page outside the pool has none
-    const auto look_up = [&](int64_t at, int64_t (&line)[U], int (&there)[U]) {
+  // scores of 16 positions, over the row's scale, in units of ln 2
+  __device__ __forceinline__ void scores(const Keys<D, kN>& key, int u, float (&x)[R][2][4]) const {
+    f32x4 N = scales<kN>(key.N);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t j = at + 16 * u;
-        const int page = j < end ? table[j >> a.cache.page_shift] : -1;
-        const bool valid = page >= 0 && page < a.cache.n_pages;
-        there[u] = valid ? int(length - j < 16 ? length - j : 16) : 0;
-        line[u] = (int64_t(valid ? page : 0) * a.cache.heads + head) * a.cache.page_size + (valid ? int(j) & page_mask : 0);
-      }
-    };
-    const auto load_keys = [&](const int64_t (&line)[U], i32x4 (&key)[U][KS], Raw (&N)[U]) {
+    for (int i = 0; i < 4; ++i) N[i] = fmaf(N[i], 0.f, N[i]);      // an infinity is a NaN: no score is -infinity but a hidden one's
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int8_t* k = a.cache.k_F + line[u] * D;
+    for (int r = 0; r < R; ++r) {
+      i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-        for (int s = 0; s < KS; ++s) key[u][s] = *reinterpret_cast<const i32x4*>(k + (key_offset + s * 64));
-        N[u] = *reinterpret_cast<const Raw*>(static_cast<const char*>(a.cache.k_N) + line[u] * kNBytes + scale_offset);
-      }
-    };
-    // Keys are read a step ahead, into the registers that the products before them have left; values while the scores are taken.
-    int64_t line[U], next_line[U];
-    int there[U], next_there[U];
-    i32x4 key[U][KS];
-    Raw key_raw[U];
-    if (begin < end) {
-      look_up(begin, line, there);
-      load_keys(line, key, key_raw);
+      for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(key.F[s], q_high[r][s], acc, 0, 0, 0);
+      acc = acc << 8;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(key.F[s], q_low[r][s], acc, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[r][u][i] = float(acc[i]) * N[i];
     }
-    for (int64_t at = begin; at < end; at += T) {
-      bool whole = at >= all_from && at + T <= all_to;
-#pragma unroll
-      for (int u = 0; u < U; ++u) whole = whole && there[u] == 16;
-      look_up(at + T, next_line, next_there);
-      Raw value_raw[U];
-      uint32_t value[U][4][VW];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int8_t* v = a.cache.v_F + line[u] * D;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) load_values<D>(v + (value_offset + i * D), value[u][i]);
-        value_raw[u] = *reinterpret_cast<const Raw*>(static_cast<const char*>(a.cache.v_N) + line[u] * kNBytes + scale_offset);
-      }
+  }
 
-      // scores, over the row's scale, in units of ln 2
-      float x[R][U][4];
+  // what the weights refer to grows; seldom
+  __device__ __forceinline__ void grow(const f32x4 (&N)[2], const float (&most)[R]) {
+    float wide = 0.f;                        // of what is finite
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        f32x4 N = scales<kN>(key_raw[u]);
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) N[i] = fmaf(N[i], 0.f, N[i]);      // an infinity is a NaN: no score is -infinity but a hidden one's
+      for (int i = 0; i < 4; ++i) wide = fmaxf(wide, fabsf(N[u][i]) < __builtin_huge_valf() ? fabsf(N[u][i]) : 0.f);
+    for (int apart = 1; apart < 64; apart <<= 1) wide = fmaxf(wide, __shfl_xor(wide, apart));
+    float wider = widest;
+    if (wide > widest) {
+      // the next power of two, within the range whose reciprocal is a normal number
+      const uint32_t up = (__float_as_uint(wide) + 0x7fffffu) & 0x7f800000u;
+      wider = __uint_as_float(up > 0x7e000000u ? 0x7e000000u : up < 0x04000000u ? 0x04000000u : up);
+    }
+    const float shrink = wider > 0.f ? widest / wider : 1.f;
+    widest = wider;
+    narrow = wider > 0.f ? 128.f / wider : 0.f;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          i32x4 acc = {0, 0, 0, 0};
+    for (int r = 0; r < R; ++r) {
+      float m = fmaxf(top[r], most[r]);
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      const float factor = m == kNegInf ? 1.f : __builtin_amdgcn_exp2f(top[r] - m);
+      top[r] = m;
+      reference[r] = m == kNegInf ? 0.f : m;
+      total[r] *= factor;
 #pragma unroll
-          for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(key[u][s], q_high[r][s], acc, 0, 0, 0);
-          acc = acc << 8;
-#pragma unroll
-          for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(key[u][s], q_low[r][s], acc, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[r][u][i] = float(acc[i]) * N[i];
-        }
-      }
-      if (at + T < end) load_keys(next_line, key, key_raw);
-      f32x4 value_N[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) value_N[u] = scales<kN>(value_raw[u]);
-      if (!whole) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int j = int(at) + 16 * u + quarter * 4 + i;
-            const bool is = quarter * 4 + i < there[u];
-            if (!is) value_N[u][i] = 0.f;
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-              if (!is || j > high[r] || j < low[r]) x[r][u][i] = kNegInf;
-          }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        line[u] = next_line[u];
-        there[u] = next_there[u];
-      }
+      for (int t = 0; t < DT; ++t) sum[r][t] *= factor * shrink;
+    }
+  }
 
-      // have the references to grow?
-      float wide = 0.f;
+  // Scores to weights, of 32 positions.  whole: all of them are there, and every row sees them.
+  __device__ __forceinline__ void weigh(float (&x)[R][2][4], f32x4 (&N)[2], int at, bool whole, int there0, int there1, int quarter) {
+    bool odd = false;
+    if (!whole) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) wide = fmaxf(wide, fabsf(value_N[u][i]));
-      float most[R];
-      bool grow = wide > widest;
+        for (int i = 0; i < 4; ++i) {
+          const int j = at + 16 * u + quarter * 4 + i;
+          const bool is = quarter * 4 + i < (u ? there1 : there0);
+          if (!is) N[u][i] = 0.f;
+          odd = odd || !(fabsf(N[u][i]) < __builtin_huge_valf());
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        most[r] = x[r][0][0];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) most[r] = fmaxf(most[r], x[r][u][i]);
-        most[r] *= q_scale[r];
-        grow = grow || most[r] > top[r] + kSlack;
-      }
-      if (__any(grow)) {
-        wide = 0.f;                          // of what is finite
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) wide = fmaxf(wide, fabsf(value_N[u][i]) < __builtin_huge_valf() ? fabsf(value_N[u][i]) : 0.f);
-        for (int apart = 1; apart < 64; apart <<= 1) wide = fmaxf(wide, __shfl_xor(wide, apart));
-        float wider = widest;
-        if (wide > widest) {
-          // the next power of two, within the range whose reciprocal is a normal number
-          const uint32_t up = (__float_as_uint(wide) + 0x7fffffu) & 0x7f800000u;
-          wider = __uint_as_float(up > 0x7e000000u ? 0x7e000000u : up < 0x04000000u ? 0x04000000u : up);
+          for (int r = 0; r < R; ++r)
+            if (!is || j > high[r] || j < low[r]) x[r][u][i] = kNegInf;
         }
-        const float shrink = wider > 0.f ? widest / wider : 1.f;
-        widest = wider;
-        narrow = wider > 0.f ? 128.f / wider : 0.f;
+      odd = __any(odd);
+    }
+    float wide = 0.f;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          float m = fmaxf(top[r], most[r]);
-          m = fmaxf(m, __shfl_xor(m, 16));
-          m = fmaxf(m, __shfl_xor(m, 32));
-          const float factor = m == kNegInf ? 1.f : __builtin_amdgcn_exp2f(top[r] - m);
-          top[r] = m;
-          reference[r] = m == kNegInf ? 0.f : m;
-          total[r] *= factor;
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int t = 0; t < DT; ++t) sum[r][t] *= factor * shrink;
-        }
-      }
-
-      // weights
-      f16x8 p[R][T / 32], p_low[R][T / 32];
+      for (int i = 0; i < 4; ++i) wide = fmaxf(wide, fabsf(N[u][i]));
+    float most[R];
+    bool more = wide > widest;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const f32x4 n = value_N[u] * narrow;
+    for (int r = 0; r < R; ++r) {
+      most[r] = x[r][0][0];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(x[r][u][i], q_scale[r], -reference[r]));
-            total[r] += e;
-            float w = e * n[i];
-            if (!whole && x[r][u][i] == kNegInf) w = 0.f;      // N may be anything there
-            const _Float16 h = _Float16(w);
-            p[r][u / 2][(u % 2) * 4 + i] = h;
-            if constexpr (kFine) p_low[r][u / 2][(u % 2) * 4 + i] = _Float16(w - float(h));
-          }
-        }
-      }
-
-      // values
+        for (int i = 0; i < 4; ++i) most[r] = fmaxf(most[r], x[r][u][i]);
+      most[r] *= q_scale[r];
+      more = more || most[r] > top[r] + kSlack;
+    }
+    if (__any(more)) grow(N, most);
 #pragma unroll
-      for (int b = 0; b < T / 32; ++b)
+    for (int u = 0; u < 2; ++u) {
+      const f32x4 n = N[u] * narrow;
 #pragma unroll
-        for (int h = 0; h < VW; ++h) {
-          u32x4 tiles[4];                  // of coefficients 4 h .. 4 h + 3: 8 positions each
+      for (int r = 0; r < R; ++r)
 #pragma unroll
-          for (int pair = 0; pair < 4; ++pair) {
-            const uint32_t w0 = value[2 * b + pair / 2][(2 * pair) % 4][h] ^ 0x80808080u;
-            const uint32_t w1 = value[2 * b + pair / 2][(2 * pair) % 4 + 1][h] ^ 0x80808080u;
-            const uint32_t lo = __builtin_amdgcn_perm(w1, w0, 0x05010400u), hi = __builtin_amdgcn_perm(w1, w0, 0x07030602u);
-            tiles[0][pair] = two_values<0>(lo);
-            tiles[1][pair] = two_values<1>(lo);
-            tiles[2][pair] = two_values<0>(hi);
-            tiles[3][pair] = two_values<1>(hi);
-          }
-#pragma unroll
-          for (int t = 0; t < (D == 32 ? 2 : 4); ++t) {
-            const f16x8 v = __builtin_bit_cast(f16x8, tiles[t]);
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-              sum[r][4 * h + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[r][b], sum[r][4 * h + t], 0, 0, 0);
-              if constexpr (kFine)
-                sum[r][4 * h + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p_low[r][b], sum[r][4 * h + t], 0, 0, 0);
-            }
-          }
+        for (int i = 0; i < 4; ++i) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(x[r][u][i], q_scale[r], -reference[r]));
+          total[r] += e;
+          const float w = e * n[i];
+          const _Float16 h = _Float16(w);
+          p[r][u * 4 + i] = h;
+          if constexpr (kFine) p_low[r][u * 4 + i] = _Float16(w - float(h));
         }
     }
+    if (odd) {                               // zero times an N that is not finite
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (x[r][i / 4][i % 4] == kNegInf) {
+            p[r][i] = _Float16(0);
+            if constexpr (kFine) p_low[r][i] = _Float16(0);
+          }
+    }
+  }
 
-    // a lane has coefficients (4 quarter + i) DT + t of its rows
+  // the weighted values of coefficient tile t
+  __device__ __forceinline__ void add(int t, f16x8 v) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      sum[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[r], sum[r][t], 0, 0, 0);
+      if constexpr (kFine) sum[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p_low[r], sum[r][t], 0, 0, 0);
+    }
+  }
+
+  // a lane has coefficients (4 quarter + i) DT + t of its rows
+  __device__ __forceinline__ void store(const AttendCall& a, int split, int quarter) {
     const float unit = widest * (1.f / (128.f * 127.f));
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -384,6 +358,86 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
         }
       }
     }
+  }
+};
+
+// The values of four neighbouring coefficients at 8 positions (their words w) as operands: tiles[t], coefficient t of the four
+__device__ __forceinline__ void value_tiles(const uint32_t (&w)[8], u32x4 (&tiles)[4]) {
+#pragma unroll
+  for (int pair = 0; pair < 4; ++pair) {
+    const uint32_t w0 = w[2 * pair] ^ 0x80808080u, w1 = w[2 * pair + 1] ^ 0x80808080u;
+    const uint32_t lo = __builtin_amdgcn_perm(w1, w0, 0x05010400u), hi = __builtin_amdgcn_perm(w1, w0, 0x07030602u);
+    tiles[0][pair] = two_values<0>(lo);
+    tiles[1][pair] = two_values<1>(lo);
+    tiles[2][pair] = two_values<0>(hi);
+    tiles[3][pair] = two_values<1>(hi);
+  }
+}
+
+// Few rows: every wave by itself, positions of its own split.  Keys are read a step ahead, into the registers that the products before
+// them have left; values while the scores are taken.
+template <int D, int R, bool kFine, int kN>
+__global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) void k_attend(const AttendCall a) {
+  constexpr int VW = D >= 64 ? D / 64 : 1;       // 32-bit words of values a lane has of a position
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, quarter = lane >> 4;
+  Part part;
+  if (!part.find(a, wave)) return;
+  const uint32_t apart = a.row_blocks * uint32_t(a.waves_rows) * (16 * R);
+  Rows<D, R, kFine, kN> rows;
+  for (uint32_t first = (part.row_block * uint32_t(a.waves_rows) + wave % a.waves_rows) * (16 * R); first < part.rows; first += apart) {
+    rows.begin(a, part, first, c, quarter);
+    const Range sees(a, part, first, part.rows - first < 16 * R ? part.rows - first : 16 * R);
+    const int64_t start = (sees.from & ~63) + int64_t(part.split) * a.chunk;
+    const int begin = start < sees.to ? int(start) : sees.to;
+    const int end = part.split == a.n_splits - 1 || start + a.chunk > sees.to ? sees.to : int(start + a.chunk);
+    Lines16 now[2], next[2];
+    Keys<D, kN> key[2];
+    if (begin < end) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        now[u].find(a, part, begin + 16 * u, end);
+        key[u].load(a, now[u].line, c, quarter);
+      }
+    }
+    for (int at = begin; at < end; at += 32) {
+      next[0].find(a, part, at + 32, end);
+      next[1].find(a, part, at + 48, end);
+      typename Scales<kN>::Raw N_raw[2];
+      uint32_t value[VW][8];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int8_t* v = a.cache.v_F + now[u].line * D;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t w[VW];
+          load_values<D>(v + uint32_t((quarter * 4 + i) * D + c * (D / 16)), w);
+#pragma unroll
+          for (int h = 0; h < VW; ++h) value[h][u * 4 + i] = w[h];
+        }
+        N_raw[u] = load_N<kN>(a.cache.v_N, now[u].line, quarter);
+      }
+      float x[R][2][4];
+      rows.scores(key[0], 0, x);
+      rows.scores(key[1], 1, x);
+      if (at + 32 < end) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) key[u].load(a, next[u].line, c, quarter);
+      }
+      f32x4 N[2] = {scales<kN>(N_raw[0]), scales<kN>(N_raw[1])};
+      const bool whole = at >= sees.all_from && at + 32 <= sees.all_to && now[0].there == 16 && now[1].there == 16;
+      rows.weigh(x, N, at, whole, now[0].there, now[1].there, quarter);
+#pragma unroll
+      for (int h = 0; h < VW; ++h) {
+        u32x4 tiles[4];
+        value_tiles(value[h], tiles);
+#pragma unroll
+        for (int t = 0; t < (D == 32 ? 2 : 4); ++t) rows.add(4 * h + t, __builtin_bit_cast(f16x8, tiles[t]));
+      }
+      now[0] = next[0];
+      now[1] = next[1];
+    }
+    rows.store(a, part.split, quarter);
   }
 }
 
