@@ -20,7 +20,9 @@ namespace pbz {
 namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -135,31 +137,35 @@ struct Range {
   }
 };
 
-// The lines of 16 positions: the first one's index, and how many there are; a page outside the pool has none.
+// The lines of 16 positions: the first one's index, and how many there are; a page outside the pool has none.  Looked up in two steps, the
+// table's entry well before it is needed (a miss of the scalar cache lasts as long as a step).
+__device__ __forceinline__ int entry(const AttendCall& a, const Part& part, int at, int end) {
+  return part.table[(at < end ? at : end - 1) >> a.cache.page_shift];
+}
 struct Lines16 {
   int64_t line;
   int there;
-  __device__ __forceinline__ void find(const AttendCall& a, const Part& part, int at, int end) {
-    const int page = at < end ? part.table[at >> a.cache.page_shift] : -1;
-    const bool valid = page >= 0 && page < a.cache.n_pages;
+  __device__ __forceinline__ void find(const AttendCall& a, const Part& part, int page, int at, int end) {
+    const bool valid = at < end && page >= 0 && page < a.cache.n_pages;
     there = valid ? (part.length - at < 16 ? part.length - at : 16) : 0;
     line = (int64_t(valid ? page : 0) * a.cache.heads + part.head) * a.cache.page_size +
            (valid ? at & (a.cache.page_size - 1) : 0);
   }
 };
 
-// Keys of 16 positions as a lane holds them, and their N.
+// Keys of 16 positions as a lane holds them, and the N of keys and values.
 template <int D, int kN>
 struct Keys {
   static constexpr int KS = D >= 64 ? D / 64 : 1;       // integer products to a line
   i32x4 F[KS];
-  typename Scales<kN>::Raw N;
+  typename Scales<kN>::Raw N, value_N;
   __device__ __forceinline__ void load(const AttendCall& a, int64_t line, int c, int quarter) {
     const int8_t* k = a.cache.k_F + line * D;
     const uint32_t offset = c * D + (D == 32 ? (quarter & 1) * 16 : quarter * 16);
 #pragma unroll
     for (int s = 0; s < KS; ++s) F[s] = *reinterpret_cast<const i32x4*>(k + (offset + s * 64));
     N = load_N<kN>(a.cache.k_N, line, quarter);
+    value_N = load_N<kN>(a.cache.v_N, line, quarter);
   }
 };
 
@@ -392,18 +398,17 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
     const int begin = start < sees.to ? int(start) : sees.to;
     const int end = part.split == a.n_splits - 1 || start + a.chunk > sees.to ? sees.to : int(start + a.chunk);
     Lines16 now[2], next[2];
+    int page[2] = {0, 0};
     Keys<D, kN> key[2];
     if (begin < end) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        now[u].find(a, part, begin + 16 * u, end);
+        now[u].find(a, part, entry(a, part, begin + 16 * u, end), begin + 16 * u, end);
         key[u].load(a, now[u].line, c, quarter);
+        page[u] = entry(a, part, begin + 32 + 16 * u, end);
       }
     }
     for (int at = begin; at < end; at += 32) {
-      next[0].find(a, part, at + 32, end);
-      next[1].find(a, part, at + 48, end);
-      typename Scales<kN>::Raw N_raw[2];
       uint32_t value[VW][8];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -415,16 +420,17 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
 #pragma unroll
           for (int h = 0; h < VW; ++h) value[h][u * 4 + i] = w[h];
         }
-        N_raw[u] = load_N<kN>(a.cache.v_N, now[u].line, quarter);
       }
+      f32x4 N[2] = {scales<kN>(key[0].value_N), scales<kN>(key[1].value_N)};
       float x[R][2][4];
       rows.scores(key[0], 0, x);
       rows.scores(key[1], 1, x);
-      if (at + 32 < end) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) key[u].load(a, next[u].line, c, quarter);
+      for (int u = 0; u < 2; ++u) {
+        next[u].find(a, part, page[u], at + 32 + 16 * u, end);
+        page[u] = entry(a, part, at + 64 + 16 * u, end);
+        if (at + 32 < end) key[u].load(a, next[u].line, c, quarter);
       }
-      f32x4 N[2] = {scales<kN>(N_raw[0]), scales<kN>(N_raw[1])};
       const bool whole = at >= sees.all_from && at + 32 <= sees.all_to && now[0].there == 16 && now[1].there == 16;
       rows.weigh(x, N, at, whole, now[0].there, now[1].there, quarter);
 #pragma unroll
@@ -441,6 +447,356 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
   }
 }
 
+// A wave's 32 rows of one head in tiles of 32: the same as Rows, a lane having one row and 16 of a step's 32 positions,
+// 8 (i / 4) + 4 half + i % 4.  Whether the weights' reference has to grow shows in their sum, which is taken anyway: a lane's part of it
+// may reach 2^8, and is infinite or no number while there is no reference.
+template <int D, bool kFine>
+struct TallRows {
+  static constexpr int KS = D / 32, DT = D / 32;
+  int64_t place;
+  int low, high;
+  i32x4 q_high[KS], q_low[KS];
+  float q_scale, minus_top, total, widest;
+  f32x16 sum[DT];
+  f16x8 p[2], p_low[2];
+
+  __device__ __forceinline__ void begin(const AttendCall& a, const Part& part, uint32_t first_row, int c, int half) {
+    const uint32_t groups = uint32_t(a.groups);
+    const uint32_t asked = first_row + c;
+    const bool there = asked < part.rows;
+    const uint32_t row = there ? asked : part.rows - 1;
+    const uint32_t token = row / groups;
+    const int64_t at = (part.first + token) * a.q_heads + int64_t(part.head) * a.groups + (row - token * groups);
+    place = there ? at : -1;
+    const int position = part.length - part.fresh + int(token);
+    high = !there ? -1 : a.causal ? position : part.length - 1;
+    low = a.window > 0 && position - int(a.window) + 1 > 0 ? position - int(a.window) + 1 : 0;
+    q_scale = a.space.q_scale[at];
+    if (q_scale == 0.f) q_scale = 0x1p-100f;             // all of the row's products are zero; a hidden one stays -infinity
+    const int8_t* q = a.space.q + at * (2 * D) + half * 16;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      q_high[s] = *reinterpret_cast<const i32x4*>(q + s * 32);
+      q_low[s] = *reinterpret_cast<const i32x4*>(q + D + s * 32);
+    }
+    minus_top = there ? -kNegInf : 0.f;
+    total = widest = 0.f;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[t][i] = 0.f;
+  }
+
+  // products of 32 positions' indices with the row's fixed-point coefficients
+  __device__ __forceinline__ i32x16 products(const i32x4 (&key)[KS]) const {
+    i32x16 acc;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[i] = 0;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(key[s], q_high[s], acc, 0, 0, 0);
+    acc = acc << 8;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(key[s], q_low[s], acc, 0, 0, 0);
+    return acc;
+  }
+
+  // the values' largest N so far is another one, by whose share the sums shrink
+  __device__ __forceinline__ void widen(float wider) {
+    const float shrink = widest / wider;
+    widest = wider;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) sum[t] *= shrink;
+  }
+
+  // exponentials against the reference; their sum
+  __device__ __forceinline__ float exponentials(const float (&x)[16], float minus, float (&e)[16]) const {
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      e[i] = __builtin_amdgcn_exp2f(fmaf(x[i], q_scale, minus));
+      part[i % 4] += e[i];
+    }
+    return (part[0] + part[1]) + (part[2] + part[3]);
+  }
+
+  // Products to weights.  key_N, N: of keys and values at the lane's positions, the latter over the largest so far and times 2^7; odd: some
+  // of them are not finite.
+  __device__ __forceinline__ void weigh(const i32x16& acc, const f32x4 (&key_N)[4], const f32x4 (&N)[4], int at, bool whole, int there0,
+                                        int there1, bool odd, int half) {
+    float x[16], e[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = float(acc[i]) * key_N[i / 4][i % 4];
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int place16 = 8 * (i / 4 % 2) + 4 * half + i % 4;
+        const int j = at + 16 * (i / 8) + place16;
+        if (place16 >= (i < 8 ? there0 : there1) || j > high || j < low) x[i] = kNegInf;
+      }
+    }
+    float more = exponentials(x, minus_top, e);
+    if (__any(!(more <= 256.f))) {
+      float most = x[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) most = fmaxf(most, x[i]);
+      most *= q_scale;
+      most = fmaxf(most, __shfl_xor(most, 32));
+      most = fmaxf(most, -minus_top);
+      const float factor = most == kNegInf ? 1.f : __builtin_amdgcn_exp2f(-minus_top - most);
+      minus_top = -most;
+      total *= factor;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) sum[t] *= factor;
+      more = exponentials(x, most == kNegInf ? 0.f : minus_top, e);
+    }
+    total += more;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float w = e[i] * N[i / 4][i % 4];
+      const _Float16 h = _Float16(w);
+      p[i / 8][i % 8] = h;
+      if constexpr (kFine) p_low[i / 8][i % 8] = _Float16(w - float(h));
+    }
+    if (!whole && odd) {                     // zero times an N that is not finite
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (x[i] == kNegInf) {
+          p[i / 8][i % 8] = _Float16(0);
+          if constexpr (kFine) p_low[i / 8][i % 8] = _Float16(0);
+        }
+    }
+  }
+
+  __device__ __forceinline__ void add(int b, int t, f16x8 v) {
+    sum[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[b], sum[t], 0, 0, 0);
+    if constexpr (kFine) sum[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p_low[b], sum[t], 0, 0, 0);
+  }
+
+  // a lane has coefficients (8 (i / 4) + 4 half + i % 4) DT + t of its row
+  __device__ __forceinline__ void store(const AttendCall& a, int split, int half) {
+    const float l = total + __shfl_xor(total, 32);
+    if (place < 0) return;
+    const float top = l != l ? 0.f : -minus_top;         // a row that sees a NaN is one, also where it sees nothing else
+    const float unit = widest * (1.f / (128.f * 127.f));
+    const int64_t to = int64_t(split) * a.n_tokens * a.q_heads + place;
+    if (half == 0) a.space.state[to] = make_float2(top, l);
+    if (top == kNegInf) return;
+    float* out = a.space.sums + to * D + half * 4 * DT;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float* o = out + (8 * (i / 4) + i % 4) * DT;
+      if constexpr (DT >= 4) {
+#pragma unroll
+        for (int t = 0; t < DT; t += 4) {
+          const f32x4 v = {sum[t][i], sum[t + 1][i], sum[t + 2][i], sum[t + 3][i]};
+          *reinterpret_cast<f32x4*>(o + t) = v * unit;
+        }
+      } else {
+        *reinterpret_cast<float2*>(o) = make_float2(sum[0][i] * unit, sum[1][i] * unit);
+      }
+    }
+  }
+};
+
+// The largest over a wave's lanes, in all of them; register moves only.
+__device__ __forceinline__ float wave_max(float v) {
+  const auto shifted = [](float x, auto control, auto rows) {
+    return __uint_as_float(uint32_t(__builtin_amdgcn_update_dpp(int(__float_as_uint(x)), int(__float_as_uint(x)), decltype(control)::value,
+                                                                decltype(rows)::value, 0xf, false)));
+  };
+  v = fmaxf(v, shifted(v, std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>()));
+  v = fmaxf(v, shifted(v, std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>()));
+  v = fmaxf(v, shifted(v, std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>()));
+  v = fmaxf(v, shifted(v, std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>()));
+  v = fmaxf(v, shifted(v, std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>()));
+  v = fmaxf(v, shifted(v, std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>()));
+  return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), 63)));
+}
+
+// Many rows: a workgroup's four waves have neighbouring row tiles and go through the positions together, 64 to a stage.  Each wave
+// converts the values of 16 of them into LDS, where every wave finds its operands, and N of all lies there, too; two buffers, so one
+// barrier to a stage.  Every load is made whether or not it will be used (behind the end: of the pool's first line), so that
+// the waits between loads and their uses count exactly.
+template <int D, bool kFine, int kN>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const AttendCall a) {
+  constexpr int DT = D / 32, KS = D / 32, VW = D >= 128 ? D / 128 : 1;
+  constexpr int kChunks = D / 16, kKeyLoads = D / 64;      // 16-byte pieces of a line; loads of 64 of them for a wave's 16 lines
+  __shared__ u32x4 operands[2][4][DT][64];
+  __shared__ i32x4 keys[3][64][kChunks];         // piece p of line l at p ^ (l >> s), so that a read of 32 lines has 8 lanes on every bank
+  __shared__ alignas(16) float scale_of[2][2][64];           // keys, values (over the largest so far, times 2^7)
+  __shared__ float2 reach[2];                    // the largest N of values so far, up to the next power of two; not 0: some N is not finite
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, half = lane >> 5;
+  Part part;
+  if (!part.find(a, 0)) return;
+  const uint32_t apart = a.row_blocks * 128;
+  TallRows<D, kFine> rows;
+  for (uint32_t first = part.row_block * 128; first < part.rows; first += apart) {
+    const Range all(a, part, first, part.rows - first < 128 ? part.rows - first : 128);
+    const int64_t start = (all.from & ~63) + int64_t(part.split) * a.chunk;
+    const int begin = start < all.to ? int(start) : all.to;
+    const int end = part.split == a.n_splits - 1 || start + a.chunk > all.to ? all.to : int(start + a.chunk);
+    const uint32_t own = first + wave * 32;
+    rows.begin(a, part, own, c, half);
+    Range sees(a, part, own < part.rows ? own : first, own < part.rows ? (part.rows - own < 32 ? part.rows - own : 32) : 1);
+    if (own >= part.rows) sees.to = 0;
+    const int own_end = sees.to < end ? sees.to : end;
+    if (begin < end) {
+      // a stage's 64 positions: this wave's 16 of the values, one N a lane; and the 32 positions of a step's keys
+      int page[4];
+      Lines16 lines[4];
+      uint32_t word[VW][8];
+      float N_next = 0.f, widest = 0.f;
+      i32x4 key_word[kKeyLoads];
+      const auto look_up = [&](int at) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) page[u] = entry(a, part, at + 16 * u, end);
+      };
+      const auto resolve = [&](int at, Lines16 (&l)[4]) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) l[u].find(a, part, page[u], at + 16 * u, end);
+      };
+      const auto own_line = [&](const Lines16 (&l)[4]) {
+        return wave == 0 ? l[0].line : wave == 1 ? l[1].line : wave == 2 ? l[2].line : l[3].line;
+      };
+      const auto load_values_of = [&](const Lines16 (&l)[4]) {
+        const int64_t mine = own_line(l);
+        const int8_t* v = a.cache.v_F + mine * D;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t offset = (8 * (i / 4) + 4 * half + i % 4) * D + c * (D / 32);
+          if constexpr (D == 64) word[0][i] = *reinterpret_cast<const uint16_t*>(v + offset);
+          else if constexpr (D == 128) word[0][i] = *reinterpret_cast<const uint32_t*>(v + offset);
+          else {
+            const uint2 u = *reinterpret_cast<const uint2*>(v + offset);
+            word[0][i] = u.x;
+            word[VW - 1][i] = u.y;
+          }
+        }
+        // waves 0 and 2 have the keys' N, the others the values'
+        const int64_t l0 = lane < 32 ? (lane < 16 ? l[0].line : l[1].line) : lane < 48 ? l[2].line : l[3].line;
+        const void* N = wave & 1 ? a.cache.v_N : a.cache.k_N;
+        const int64_t at = l0 + (lane & 15);
+        if constexpr (kN == PBZ_F32) N_next = static_cast<const float*>(N)[at];
+        else if constexpr (kN == PBZ_BF16) N_next = bf16_bits_to_float(static_cast<const uint16_t*>(N)[at]);
+        else N_next = float(static_cast<const _Float16*>(N)[at]);
+      };
+      const auto convert = [&](int buffer) {
+#pragma unroll
+        for (int h = 0; h < VW; ++h) {
+          u32x4 tiles[4];
+          value_tiles(word[h], tiles);
+#pragma unroll
+          for (int t = 0; t < (D == 64 ? 2 : 4); ++t) operands[buffer][wave][4 * h + t][lane] = tiles[t];
+        }
+        if (wave == 0) scale_of[buffer][0][lane] = fmaf(N_next, 0.f, N_next);      // an infinity is a NaN: no score is -infinity but a hidden one's
+        if (wave == 1) {
+          const int there = lane < 32 ? (lane < 16 ? lines[0].there : lines[1].there) : lane < 48 ? lines[2].there : lines[3].there;
+          const float N = (lane & 15) < there ? N_next : 0.f;
+          const bool finite = fabsf(N) < __builtin_huge_valf();
+          const float wide = wave_max(finite ? fabsf(N) : 0.f);
+          if (wide > widest) {
+            // the next power of two, within the range whose reciprocal is a normal number
+            const uint32_t up = (__float_as_uint(wide) + 0x7fffffu) & 0x7f800000u;
+            widest = __uint_as_float(up > 0x7e000000u ? 0x7e000000u : up < 0x04000000u ? 0x04000000u : up);
+          }
+          scale_of[buffer][1][lane] = widest > 0.f ? N * (128.f / widest) : N;
+          const bool odd = __any(!finite);
+          if (lane == 0) reach[buffer] = make_float2(widest, odd ? 1.f : 0.f);
+        }
+      };
+      const auto load_keys = [&](const Lines16 (&l)[4]) {
+        const i32x4* k = reinterpret_cast<const i32x4*>(a.cache.k_F + own_line(l) * D);
+#pragma unroll
+        for (int i = 0; i < kKeyLoads; ++i) key_word[i] = k[i * 64 + lane];
+      };
+      constexpr int kShift = D == 64 ? 2 : D == 128 ? 1 : 0;
+      const auto put_keys = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < kKeyLoads; ++i) {
+          const int l = 16 * wave + (i * 64 + lane) / kChunks, piece = lane % kChunks;
+          keys[buffer][l][piece ^ ((l >> kShift) & (kChunks - 1))] = key_word[i];
+        }
+      };
+      const auto products = [&](int buffer, int b) {
+        i32x4 key[KS];
+        const int l = 32 * b + c;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) key[s] = keys[buffer][l][(2 * s + half) ^ ((l >> kShift) & (kChunks - 1))];
+        return rows.products(key);
+      };
+      // What a step takes from LDS is asked for well before it is used: N before the next step's products, half of the values before the
+      // weights are made.
+      f32x4 key_N[4], N[4];
+      const auto read_N = [&](int buffer, int b) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          key_N[g] = *reinterpret_cast<const f32x4*>(&scale_of[buffer][0][32 * b + 8 * g + 4 * half]);
+          N[g] = *reinterpret_cast<const f32x4*>(&scale_of[buffer][1][32 * b + 8 * g + 4 * half]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      const auto step = [&](const i32x16& acc, int at, int buffer, int b, int there0, int there1, bool odd) {
+        if (!(at < own_end && at + 32 > sees.from)) return;
+        const bool whole = at >= sees.all_from && at + 32 <= sees.all_to && there0 == 16 && there1 == 16;
+        u32x4 early[DT], late[DT];
+#pragma unroll
+        for (int t = 0; t < DT; ++t) early[t] = operands[buffer][2 * b][t][lane];
+        __builtin_amdgcn_sched_barrier(0);
+        rows.weigh(acc, key_N, N, at, whole, there0, there1, odd, half);
+#pragma unroll
+        for (int t = 0; t < DT; ++t) late[t] = operands[buffer][2 * b + 1][t][lane];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < DT; ++t) rows.add(0, t, __builtin_bit_cast(f16x8, early[t]));
+#pragma unroll
+        for (int t = 0; t < DT; ++t) rows.add(1, t, __builtin_bit_cast(f16x8, late[t]));
+      };
+      // Keys are a stage further ahead than values: the products of a step are taken while the weights of the one before are.
+      Lines16 after[4];
+      look_up(begin);
+      resolve(begin, lines);
+      load_keys(lines);
+      load_values_of(lines);
+      look_up(begin + 64);
+      put_keys(0);
+      convert(0);
+      resolve(begin + 64, after);
+      load_keys(after);
+      look_up(begin + 128);
+      put_keys(1);
+      __syncthreads();
+      i32x16 acc = products(0, 0);
+      int buffer = 0, key_buffer = 0;
+      for (int stage = begin; stage < end; stage += 64) {
+        const int there0 = lines[0].there, there1 = lines[1].there, there2 = lines[2].there, there3 = lines[3].there;
+        const int next_buffer = key_buffer == 2 ? 0 : key_buffer + 1, free_buffer = next_buffer == 2 ? 0 : next_buffer + 1;
+        const float2 reached = reach[buffer];
+        if (reached.x > rows.widest) rows.widen(reached.x);
+        const bool odd = reached.y != 0.f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) lines[u] = after[u];
+        load_values_of(lines);
+        resolve(stage + 128, after);
+        load_keys(after);
+        look_up(stage + 192);
+        read_N(buffer, 0);
+        const i32x16 second = products(key_buffer, 1);
+        step(acc, stage, buffer, 0, there0, there1, odd);
+        read_N(buffer, 1);
+        acc = products(next_buffer, 0);
+        step(second, stage + 32, buffer, 1, there2, there3, odd);
+        buffer ^= 1;
+        key_buffer = next_buffer;
+        put_keys(free_buffer);
+        convert(buffer);
+        __syncthreads();
+      }
+    }
+    rows.store(a, part.split, half);
+  }
+}
+
 template <int D, int kN>
 int launch(int rows, bool fine, const AttendCall& call, hipStream_t s) {
   const dim3 grid((call.blocks + 7) / 8 * 8), block(256);
@@ -448,6 +804,13 @@ int launch(int rows, bool fine, const AttendCall& call, hipStream_t s) {
     if (fine) k_attend<D, 1, true, kN><<<grid, block, 0, s>>>(call);
     else k_attend<D, 1, false, kN><<<grid, block, 0, s>>>(call);
   } else {
+    if constexpr (D >= 64) {
+      if (call.waves_rows == 4) {
+        if (fine) k_attend_tall<D, true, kN><<<grid, block, 0, s>>>(call);
+        else k_attend_tall<D, false, kN><<<grid, block, 0, s>>>(call);
+        return hip_status(hipGetLastError());
+      }
+    }
     if (fine) k_attend<D, 2, true, kN><<<grid, block, 0, s>>>(call);
     else k_attend<D, 2, false, kN><<<grid, block, 0, s>>>(call);
   }
