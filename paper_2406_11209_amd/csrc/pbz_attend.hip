@@ -90,7 +90,7 @@ __device__ __forceinline__ uint32_t work_index(uint32_t blocks) {
 struct Part {
   int head, split;
   uint32_t row_block;
-  int64_t first;           // first row of q
+  int64_t seq, first;      // sequence, its first row of q
   int fresh, length;       // new tokens, positions
   uint32_t rows;           // query rows: new tokens times query heads of the head
   // (the constant address space: uniform reads through the scalar cache)
@@ -103,7 +103,7 @@ struct Part {
     const uint32_t split_block = work / a.row_blocks % a.split_blocks;
     const uint32_t head_of_all = work / a.row_blocks / a.split_blocks;
     head = int(head_of_all % uint32_t(a.cache.heads));
-    const int64_t seq = head_of_all / uint32_t(a.cache.heads);
+    seq = head_of_all / uint32_t(a.cache.heads);
     split = int(split_block) * (4 / a.waves_rows) + wave / a.waves_rows;
     if (split >= a.n_splits) return false;
     int64_t last = seq + 1;
@@ -487,17 +487,17 @@ struct TallRows {
       for (int i = 0; i < 16; ++i) sum[t][i] = 0.f;
   }
 
-  // products of 32 positions' indices with the row's fixed-point coefficients
-  __device__ __forceinline__ i32x16 products(const i32x4 (&key)[KS]) const {
-    i32x16 acc;
+  // products of 32 positions' indices with the row's fixed-point coefficients: the high bytes, then the low ones added to 256 times that
+  __device__ __forceinline__ void products_high(const i32x4 (&key)[KS], i32x16& acc) const {
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[i] = 0;
 #pragma unroll
     for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(key[s], q_high[s], acc, 0, 0, 0);
+  }
+  __device__ __forceinline__ void products_low(const i32x4 (&key)[KS], i32x16& acc) const {
     acc = acc << 8;
 #pragma unroll
     for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(key[s], q_low[s], acc, 0, 0, 0);
-    return acc;
   }
 
   // the values' largest N so far is another one, by whose share the sums shrink
@@ -519,22 +519,21 @@ struct TallRows {
     return (part[0] + part[1]) + (part[2] + part[3]);
   }
 
-  // Products to weights.  key_N, N: of keys and values at the lane's positions, the latter over the largest so far and times 2^7; odd: some
-  // of them are not finite.
-  __device__ __forceinline__ void weigh(const i32x16& acc, const f32x4 (&key_N)[4], const f32x4 (&N)[4], int at, bool whole, int there0,
-                                        int there1, bool odd, int half) {
-    float x[16], e[16];
+  // Scores over the row's scale, in units of ln 2; hidden ones are -infinity where not the whole step is seen.
+  __device__ __forceinline__ void scores(const i32x16& acc, const f32x4 (&key_N)[4], int at, bool whole, uint32_t there, int half,
+                                         float (&x)[16]) const {
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = float(acc[i]) * key_N[i / 4][i % 4];
     if (!whole) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int place16 = 8 * (i / 4 % 2) + 4 * half + i % 4;
-        const int j = at + 16 * (i / 8) + place16;
-        if (place16 >= (i < 8 ? there0 : there1) || j > high || j < low) x[i] = kNegInf;
+        const int place32 = 8 * (i / 4) + 4 * half + i % 4;
+        if (!((there >> place32) & 1) || at + place32 > high || at + place32 < low) x[i] = kNegInf;
       }
     }
-    float more = exponentials(x, minus_top, e);
+  }
+  // e: the exponentials against the reference; more: their sum.  Where that does not do, a new reference and exponentials against that.
+  __device__ __forceinline__ void refer(const float (&x)[16], float (&e)[16], float more) {
     if (__any(!(more <= 256.f))) {
       float most = x[0];
 #pragma unroll
@@ -550,6 +549,9 @@ struct TallRows {
       more = exponentials(x, most == kNegInf ? 0.f : minus_top, e);
     }
     total += more;
+  }
+  // The weights.  N: of values, over the largest so far and times 2^7; odd: some are hidden, and some N are not finite.
+  __device__ __forceinline__ void weights(const float (&x)[16], const float (&e)[16], const f32x4 (&N)[4], bool odd) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float w = e[i] * N[i / 4][i % 4];
@@ -557,7 +559,7 @@ struct TallRows {
       p[i / 8][i % 8] = h;
       if constexpr (kFine) p_low[i / 8][i % 8] = _Float16(w - float(h));
     }
-    if (!whole && odd) {                     // zero times an N that is not finite
+    if (odd) {                               // zero times an N that is not finite
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (x[i] == kNegInf) {
@@ -613,6 +615,24 @@ __device__ __forceinline__ float wave_max(float v) {
   return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), 63)));
 }
 
+// A stage of 64 positions: a lane's line (its first one where there is none), and which positions there are.
+struct Stage {
+  int64_t line;
+  uint64_t there;
+  __device__ __forceinline__ void find(const AttendCall& a, const Part& part, int page, int at, int end, int lane) {
+    const int j = at + lane;
+    const bool valid = (j & ~15) < end && j < part.length && page >= 0 && page < a.cache.n_pages;
+    line = (int64_t(valid ? page : 0) * a.cache.heads + part.head) * a.cache.page_size + (valid ? j & (a.cache.page_size - 1) : 0);
+    there = __ballot(valid);
+  }
+  // the first line of 16 positions: those behind the end may be of another page, or none, but there are as many lines to read
+  __device__ __forceinline__ int64_t first(int of) const {
+    const uint32_t lo = uint32_t(__builtin_amdgcn_readlane(int(uint32_t(line)), 16 * of));
+    const uint32_t hi = uint32_t(__builtin_amdgcn_readlane(int(uint32_t(uint64_t(line) >> 32)), 16 * of));
+    return int64_t(uint64_t(lo) | (uint64_t(hi) << 32));
+  }
+};
+
 // Many rows: a workgroup's four waves have neighbouring row tiles and go through the positions together, 64 to a stage.  Each wave
 // converts the values of 16 of them into LDS, where every wave finds its operands, and N of all lies there, too; two buffers, so one
 // barrier to a stage.  Every load is made whether or not it will be used (behind the end: of the pool's first line), so that
@@ -638,30 +658,21 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
     const int end = part.split == a.n_splits - 1 || start + a.chunk > all.to ? all.to : int(start + a.chunk);
     const uint32_t own = first + wave * 32;
     rows.begin(a, part, own, c, half);
-    Range sees(a, part, own < part.rows ? own : first, own < part.rows ? (part.rows - own < 32 ? part.rows - own : 32) : 1);
-    if (own >= part.rows) sees.to = 0;
-    const int own_end = sees.to < end ? sees.to : end;
+    const Range sees(a, part, own < part.rows ? own : first, own < part.rows ? (part.rows - own < 32 ? part.rows - own : 32) : 1);
     if (begin < end) {
+      const int32_t* table = a.table + part.seq * a.table_stride;
       // a stage's 64 positions: this wave's 16 of the values, one N a lane; and the 32 positions of a step's keys
-      int page[4];
-      Lines16 lines[4];
+      int page;                              // the table's entry for the lane's position (a vector load: waits for LDS wait for
+                                             // scalar loads, too)
       uint32_t word[VW][8];
       float N_next = 0.f, widest = 0.f;
       i32x4 key_word[kKeyLoads];
       const auto look_up = [&](int at) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) page[u] = entry(a, part, at + 16 * u, end);
+        const int j = at + lane;
+        page = table[(j < end ? j : end - 1) >> a.cache.page_shift];
       };
-      const auto resolve = [&](int at, Lines16 (&l)[4]) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) l[u].find(a, part, page[u], at + 16 * u, end);
-      };
-      const auto own_line = [&](const Lines16 (&l)[4]) {
-        return wave == 0 ? l[0].line : wave == 1 ? l[1].line : wave == 2 ? l[2].line : l[3].line;
-      };
-      const auto load_values_of = [&](const Lines16 (&l)[4]) {
-        const int64_t mine = own_line(l);
-        const int8_t* v = a.cache.v_F + mine * D;
+      const auto load_values_of = [&](const Stage& stage) {
+        const int8_t* v = a.cache.v_F + stage.first(wave) * D;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const uint32_t offset = (8 * (i / 4) + 4 * half + i % 4) * D + c * (D / 32);
@@ -673,15 +684,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
             word[VW - 1][i] = u.y;
           }
         }
-        // waves 0 and 2 have the keys' N, the others the values'
-        const int64_t l0 = lane < 32 ? (lane < 16 ? l[0].line : l[1].line) : lane < 48 ? l[2].line : l[3].line;
+        // waves 0 and 2 read the keys' N, the others the values'
         const void* N = wave & 1 ? a.cache.v_N : a.cache.k_N;
-        const int64_t at = l0 + (lane & 15);
-        if constexpr (kN == PBZ_F32) N_next = static_cast<const float*>(N)[at];
-        else if constexpr (kN == PBZ_BF16) N_next = bf16_bits_to_float(static_cast<const uint16_t*>(N)[at]);
-        else N_next = float(static_cast<const _Float16*>(N)[at]);
+        if constexpr (kN == PBZ_F32) N_next = static_cast<const float*>(N)[stage.line];
+        else if constexpr (kN == PBZ_BF16) N_next = bf16_bits_to_float(static_cast<const uint16_t*>(N)[stage.line]);
+        else N_next = float(static_cast<const _Float16*>(N)[stage.line]);
       };
-      const auto convert = [&](int buffer) {
+      const auto convert = [&](int buffer, uint64_t there) {
 #pragma unroll
         for (int h = 0; h < VW; ++h) {
           u32x4 tiles[4];
@@ -691,8 +700,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
         }
         if (wave == 0) scale_of[buffer][0][lane] = fmaf(N_next, 0.f, N_next);      // an infinity is a NaN: no score is -infinity but a hidden one's
         if (wave == 1) {
-          const int there = lane < 32 ? (lane < 16 ? lines[0].there : lines[1].there) : lane < 48 ? lines[2].there : lines[3].there;
-          const float N = (lane & 15) < there ? N_next : 0.f;
+          const float N = (there >> lane) & 1 ? N_next : 0.f;
           const bool finite = fabsf(N) < __builtin_huge_valf();
           const float wide = wave_max(finite ? fabsf(N) : 0.f);
           if (wide > widest) {
@@ -705,8 +713,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
           if (lane == 0) reach[buffer] = make_float2(widest, odd ? 1.f : 0.f);
         }
       };
-      const auto load_keys = [&](const Lines16 (&l)[4]) {
-        const i32x4* k = reinterpret_cast<const i32x4*>(a.cache.k_F + own_line(l) * D);
+      const auto load_keys = [&](const Stage& stage) {
+        const i32x4* k = reinterpret_cast<const i32x4*>(a.cache.k_F + stage.first(wave) * D);
 #pragma unroll
         for (int i = 0; i < kKeyLoads; ++i) key_word[i] = k[i * 64 + lane];
       };
@@ -718,78 +726,81 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
           keys[buffer][l][piece ^ ((l >> kShift) & (kChunks - 1))] = key_word[i];
         }
       };
-      const auto products = [&](int buffer, int b) {
-        i32x4 key[KS];
+      const auto read_keys = [&](int buffer, int b, i32x4 (&key)[KS]) {
         const int l = 32 * b + c;
 #pragma unroll
         for (int s = 0; s < KS; ++s) key[s] = keys[buffer][l][(2 * s + half) ^ ((l >> kShift) & (kChunks - 1))];
-        return rows.products(key);
       };
-      // What a step takes from LDS is asked for well before it is used: N before the next step's products, half of the values before the
-      // weights are made.
-      f32x4 key_N[4], N[4];
-      const auto read_N = [&](int buffer, int b) {
+      // A step: its weights and weighted values, and meanwhile the products of the next one (of keys 32 next_b .. of a buffer), so that
+      // the matrix cores have work while exponentials are taken.
+      const auto step = [&](i32x16& acc, int at, int buffer, int b, int next_keys, int next_b, uint32_t there, bool odd) {
+        const bool whole = at >= sees.all_from && at + 32 <= sees.all_to && there == ~0u;
+        f32x4 key_N[4], N[4];
+        i32x4 key[KS];
+        float x[16], e[16];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          key_N[g] = *reinterpret_cast<const f32x4*>(&scale_of[buffer][0][32 * b + 8 * g + 4 * half]);
-          N[g] = *reinterpret_cast<const f32x4*>(&scale_of[buffer][1][32 * b + 8 * g + 4 * half]);
+        for (int g = 0; g < 4; ++g) key_N[g] = *reinterpret_cast<const f32x4*>(&scale_of[buffer][0][32 * b + 8 * g + 4 * half]);
+        read_keys(next_keys, next_b, key);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) N[g] = *reinterpret_cast<const f32x4*>(&scale_of[buffer][1][32 * b + 8 * g + 4 * half]);
+        rows.scores(acc, key_N, at, whole, there, half, x);
+        rows.products_high(key, acc);
+        const float more = rows.exponentials(x, rows.minus_top, e);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {       // a product, then a share of the exponentials
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x002, 48 / KS, 0);
         }
-        __builtin_amdgcn_sched_barrier(0);
-      };
-      const auto step = [&](const i32x16& acc, int at, int buffer, int b, int there0, int there1, bool odd) {
-        if (!(at < own_end && at + 32 > sees.from)) return;
-        const bool whole = at >= sees.all_from && at + 32 <= sees.all_to && there0 == 16 && there1 == 16;
-        u32x4 early[DT], late[DT];
+        rows.refer(x, e, more);
+        u32x4 tile[DT];
 #pragma unroll
-        for (int t = 0; t < DT; ++t) early[t] = operands[buffer][2 * b][t][lane];
-        __builtin_amdgcn_sched_barrier(0);
-        rows.weigh(acc, key_N, N, at, whole, there0, there1, odd, half);
+        for (int t = 0; t < DT; ++t) tile[t] = operands[buffer][2 * b][t][lane];
+        rows.products_low(key, acc);
+        rows.weights(x, e, N, !whole && odd);
 #pragma unroll
-        for (int t = 0; t < DT; ++t) late[t] = operands[buffer][2 * b + 1][t][lane];
-        __builtin_amdgcn_sched_barrier(0);
+        for (int t = 0; t < DT; ++t) rows.add(0, t, __builtin_bit_cast(f16x8, tile[t]));
 #pragma unroll
-        for (int t = 0; t < DT; ++t) rows.add(0, t, __builtin_bit_cast(f16x8, early[t]));
-#pragma unroll
-        for (int t = 0; t < DT; ++t) rows.add(1, t, __builtin_bit_cast(f16x8, late[t]));
+        for (int t = 0; t < DT; ++t) rows.add(1, t, __builtin_bit_cast(f16x8, operands[buffer][2 * b + 1][t][lane]));
       };
       // Keys are a stage further ahead than values: the products of a step are taken while the weights of the one before are.
-      Lines16 after[4];
+      Stage now, after;
       look_up(begin);
-      resolve(begin, lines);
-      load_keys(lines);
-      load_values_of(lines);
+      now.find(a, part, page, begin, end, lane);
+      load_keys(now);
+      load_values_of(now);
       look_up(begin + 64);
       put_keys(0);
-      convert(0);
-      resolve(begin + 64, after);
+      convert(0, now.there);
+      after.find(a, part, page, begin + 64, end, lane);
       load_keys(after);
       look_up(begin + 128);
       put_keys(1);
       __syncthreads();
-      i32x16 acc = products(0, 0);
+      i32x16 acc;
+      {
+        i32x4 key[KS];
+        read_keys(0, 0, key);
+        rows.products_high(key, acc);
+        rows.products_low(key, acc);
+      }
       int buffer = 0, key_buffer = 0;
       for (int stage = begin; stage < end; stage += 64) {
-        const int there0 = lines[0].there, there1 = lines[1].there, there2 = lines[2].there, there3 = lines[3].there;
         const int next_buffer = key_buffer == 2 ? 0 : key_buffer + 1, free_buffer = next_buffer == 2 ? 0 : next_buffer + 1;
         const float2 reached = reach[buffer];
         if (reached.x > rows.widest) rows.widen(reached.x);
         const bool odd = reached.y != 0.f;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) lines[u] = after[u];
-        load_values_of(lines);
-        resolve(stage + 128, after);
+        const uint64_t there = now.there;
+        now = after;
+        load_values_of(now);
+        after.find(a, part, page, stage + 128, end, lane);
         load_keys(after);
         look_up(stage + 192);
-        read_N(buffer, 0);
-        const i32x16 second = products(key_buffer, 1);
-        step(acc, stage, buffer, 0, there0, there1, odd);
-        read_N(buffer, 1);
-        acc = products(next_buffer, 0);
-        step(second, stage + 32, buffer, 1, there2, there3, odd);
+        step(acc, stage, buffer, 0, key_buffer, 1, uint32_t(there), odd);
+        step(acc, stage + 32, buffer, 1, next_buffer, 0, uint32_t(there >> 32), odd);
         buffer ^= 1;
         key_buffer = next_buffer;
         put_keys(free_buffer);
-        convert(buffer);
+        convert(buffer, now.there);
         __syncthreads();
       }
     }
