@@ -88,7 +88,7 @@ __device__ __forceinline__ uint32_t work_index(uint32_t blocks) {
 
 // What a workgroup works on: a sequence's rows and positions, cut to what the arrays have, and a head of the cache.
 struct Part {
-  int head, split;
+  int head, split, record;
   uint32_t row_block;
   int64_t seq, first;      // sequence, its first row of q
   int fresh, length;       // new tokens, positions
@@ -104,8 +104,8 @@ struct Part {
     const uint32_t head_of_all = work / a.row_blocks / a.split_blocks;
     head = int(head_of_all % uint32_t(a.cache.heads));
     seq = head_of_all / uint32_t(a.cache.heads);
-    split = int(split_block) * (4 / a.waves_rows) + wave / a.waves_rows;
-    if (split >= a.n_splits) return false;
+    record = int(split_block);
+    split = record * (4 / a.waves_rows) + wave / a.waves_rows;
     int64_t last = seq + 1;
     first = seq;
     if (a.starts) {
@@ -337,9 +337,44 @@ struct Rows {
     }
   }
 
-  // a lane has coefficients (4 quarter + i) DT + t of its rows
-  __device__ __forceinline__ void store(const AttendCall& a, int split, int quarter) {
+  // What a wave leaves for another with the same rows: per lane references, totals, sums in one unit; the lanes of a wave side by side.
+  static constexpr int kLeft = R * (2 + 4 * DT);
+  __device__ __forceinline__ void leave(float* left, int lane) const {
     const float unit = widest * (1.f / (128.f * 127.f));
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      left[(2 * r) * 64 + lane] = top[r];
+      left[(2 * r + 1) * 64 + lane] = total[r];
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) left[(2 * R + (r * DT + t) * 4 + i) * 64 + lane] = sum[r][t][i] * unit;
+    }
+  }
+  __device__ __forceinline__ void into_unit() {
+    const float unit = widest * (1.f / (128.f * 127.f));
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int t = 0; t < DT; ++t) sum[r][t] *= unit;
+  }
+  __device__ __forceinline__ void take(const float* left, int lane) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const float other = left[(2 * r) * 64 + lane], both = fmaxf(top[r], other);
+      const float mine = both == kNegInf ? 1.f : __builtin_amdgcn_exp2f(top[r] - both);
+      const float theirs = both == kNegInf ? 1.f : __builtin_amdgcn_exp2f(other - both);
+      top[r] = both;
+      total[r] = total[r] * mine + left[(2 * r + 1) * 64 + lane] * theirs;
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[r][t][i] = sum[r][t][i] * mine + left[(2 * R + (r * DT + t) * 4 + i) * 64 + lane] * theirs;
+    }
+  }
+
+  // a lane has coefficients (4 quarter + i) DT + t of its rows
+  __device__ __forceinline__ void store(const AttendCall& a, int record, int quarter) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float l = total[r];
@@ -347,7 +382,7 @@ struct Rows {
       l += __shfl_xor(l, 32);
       if (place[r] < 0) continue;
       if (l != l) top[r] = 0.f;            // a row that sees a NaN is one, also where it sees nothing else
-      const int64_t to = int64_t(split) * a.n_tokens * a.q_heads + place[r];
+      const int64_t to = int64_t(record) * a.n_tokens * a.q_heads + place[r];
       if (quarter == 0) a.space.state[to] = make_float2(top[r], l);
       if (top[r] == kNegInf) continue;
       float* out = a.space.sums + to * D + quarter * 4 * DT;
@@ -357,10 +392,10 @@ struct Rows {
 #pragma unroll
           for (int t = 0; t < DT; t += 4) {
             const f32x4 v = {sum[r][t][i], sum[r][t + 1][i], sum[r][t + 2][i], sum[r][t + 3][i]};
-            *reinterpret_cast<f32x4*>(out + i * DT + t) = v * unit;
+            *reinterpret_cast<f32x4*>(out + i * DT + t) = v;
           }
         } else {
-          *reinterpret_cast<float2*>(out + i * DT) = make_float2(sum[r][0][i] * unit, sum[r][1][i] * unit);
+          *reinterpret_cast<float2*>(out + i * DT) = make_float2(sum[r][0][i], sum[r][1][i]);
         }
       }
     }
@@ -380,7 +415,7 @@ __device__ __forceinline__ void value_tiles(const uint32_t (&w)[8], u32x4 (&tile
   }
 }
 
-// Few rows: every wave by itself, positions of its own split.  Keys are read a step ahead, into the registers that the products before
+// Few rows: every wave by itself, positions of its own split; waves with the same rows join what they have before it is stored.  Keys are read a step ahead, into the registers that the products before
 // them have left; values while the scores are taken.
 template <int D, int R, bool kFine, int kN>
 __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) void k_attend(const AttendCall a) {
@@ -389,14 +424,18 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
   const int c = lane & 15, quarter = lane >> 4;
   Part part;
   if (!part.find(a, wave)) return;
-  const uint32_t apart = a.row_blocks * uint32_t(a.waves_rows) * (16 * R);
+  const int sharing = 4 / a.waves_rows;          // waves with the same rows, whose splits become one record
   Rows<D, R, kFine, kN> rows;
-  for (uint32_t first = (part.row_block * uint32_t(a.waves_rows) + wave % a.waves_rows) * (16 * R); first < part.rows; first += apart) {
+  __shared__ float left[3][Rows<D, R, kFine, kN>::kLeft * 64];
+  const uint32_t together = uint32_t(a.waves_rows) * (16 * R);
+  for (uint32_t base = part.row_block * together; base < part.rows; base += a.row_blocks * together) {
+    const uint32_t first = base + uint32_t(wave % a.waves_rows) * (16 * R);
+    const bool any = first < part.rows;
     rows.begin(a, part, first, c, quarter);
-    const Range sees(a, part, first, part.rows - first < 16 * R ? part.rows - first : 16 * R);
+    const Range sees(a, part, any ? first : base, any && part.rows - first < 16 * R ? part.rows - first : any ? 16 * R : 1);
     const int64_t start = (sees.from & ~63) + int64_t(part.split) * a.chunk;
     const int begin = start < sees.to ? int(start) : sees.to;
-    const int end = part.split == a.n_splits - 1 || start + a.chunk > sees.to ? sees.to : int(start + a.chunk);
+    const int end = !any || part.split >= a.n_splits ? begin : part.split == a.n_splits - 1 || start + a.chunk > sees.to ? sees.to : int(start + a.chunk);
     Lines16 now[2], next[2];
     int page[2] = {0, 0};
     Keys<D, kN> key[2];
@@ -443,7 +482,17 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
       now[0] = next[0];
       now[1] = next[1];
     }
-    rows.store(a, part.split, quarter);
+    const int turn = wave / a.waves_rows;
+    if (sharing > 1) {
+      if (turn > 0) rows.leave(left[wave - a.waves_rows], lane);
+      __syncthreads();
+    }
+    if (turn == 0) {
+      rows.into_unit();
+      for (int w = 1; w < sharing; ++w) rows.take(left[wave + (w - 1) * a.waves_rows], lane);
+      rows.store(a, part.record, quarter);
+    }
+    if (sharing > 1) __syncthreads();
   }
 }
 
@@ -575,12 +624,12 @@ struct TallRows {
   }
 
   // a lane has coefficients (8 (i / 4) + 4 half + i % 4) DT + t of its row
-  __device__ __forceinline__ void store(const AttendCall& a, int split, int half) {
+  __device__ __forceinline__ void store(const AttendCall& a, int record, int half) {
     const float l = total + __shfl_xor(total, 32);
     if (place < 0) return;
     const float top = l != l ? 0.f : -minus_top;         // a row that sees a NaN is one, also where it sees nothing else
     const float unit = widest * (1.f / (128.f * 127.f));
-    const int64_t to = int64_t(split) * a.n_tokens * a.q_heads + place;
+    const int64_t to = int64_t(record) * a.n_tokens * a.q_heads + place;
     if (half == 0) a.space.state[to] = make_float2(top, l);
     if (top == kNegInf) return;
     float* out = a.space.sums + to * D + half * 4 * DT;
@@ -804,7 +853,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
         __syncthreads();
       }
     }
-    rows.store(a, part.split, half);
+    rows.store(a, part.record, half);
   }
 }
 

@@ -15,27 +15,27 @@ constexpr int kMaxSplits = 256;
 constexpr int64_t kComputeWaves = 2048;      // waves that keep the chip busy: two to a SIMD
 constexpr int kPairsPerLaunch = 256;
 
-// 32 neighbouring elements as T; `wide`: the address is a multiple of 16 bytes
+// 16 neighbouring elements as T; `wide`: the address is a multiple of 16 bytes
 template <typename T>
-__device__ __forceinline__ void load_run(const void* p, int type, int64_t at, bool wide, T (&v)[32]) {
+__device__ __forceinline__ void load_run(const void* p, int type, int64_t at, bool wide, T (&v)[16]) {
   if (type == PBZ_F64) {
     const double* x = static_cast<const double*>(p) + at;
     if (wide) {
 #pragma unroll
-      for (int i = 0; i < 32; i += 2) {
+      for (int i = 0; i < 16; i += 2) {
         const double2 u = *reinterpret_cast<const double2*>(x + i);
         v[i] = T(u.x);
         v[i + 1] = T(u.y);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] = T(x[i]);
+      for (int i = 0; i < 16; ++i) v[i] = T(x[i]);
     }
   } else if (type == PBZ_F32) {
     const float* x = static_cast<const float*>(p) + at;
     if (wide) {
 #pragma unroll
-      for (int i = 0; i < 32; i += 4) {
+      for (int i = 0; i < 16; i += 4) {
         const float4 u = *reinterpret_cast<const float4*>(x + i);
         v[i] = T(u.x);
         v[i + 1] = T(u.y);
@@ -44,14 +44,14 @@ __device__ __forceinline__ void load_run(const void* p, int type, int64_t at, bo
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] = T(x[i]);
+      for (int i = 0; i < 16; ++i) v[i] = T(x[i]);
     }
   } else {
     const uint16_t* x = static_cast<const uint16_t*>(p) + at;
-    uint32_t w[16];
+    uint32_t w[8];
     if (wide) {
 #pragma unroll
-      for (int i = 0; i < 16; i += 4) {
+      for (int i = 0; i < 8; i += 4) {
         const uint4 u = *reinterpret_cast<const uint4*>(x + 2 * i);
         w[i] = u.x;
         w[i + 1] = u.y;
@@ -60,17 +60,17 @@ __device__ __forceinline__ void load_run(const void* p, int type, int64_t at, bo
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) w[i] = uint32_t(x[2 * i]) | (uint32_t(x[2 * i + 1]) << 16);
+      for (int i = 0; i < 8; ++i) w[i] = uint32_t(x[2 * i]) | (uint32_t(x[2 * i + 1]) << 16);
     }
     if (type == PBZ_BF16) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < 8; ++i) {
         v[2 * i] = T(__uint_as_float(w[i] << 16));
         v[2 * i + 1] = T(__uint_as_float(w[i] & 0xffff0000u));
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < 8; ++i) {
         v[2 * i] = T(float(__builtin_bit_cast(_Float16, uint16_t(w[i]))));
         v[2 * i + 1] = T(float(__builtin_bit_cast(_Float16, uint16_t(w[i] >> 16))));
       }
@@ -80,19 +80,19 @@ __device__ __forceinline__ void load_run(const void* p, int type, int64_t at, bo
 
 // the largest magnitude of a line, and whether all of its values are finite: the same in its L lanes
 template <typename T, int L>
-__device__ __forceinline__ T line_max(const T (&v)[32]) {
+__device__ __forceinline__ T line_max(const T (&v)[16]) {
   T most = T(0);
 #pragma unroll
-  for (int i = 0; i < 32; ++i) most = fmax(most, fabs(v[i]));
+  for (int i = 0; i < 16; ++i) most = fmax(most, fabs(v[i]));
 #pragma unroll
   for (int apart = 1; apart < L; apart <<= 1) most = fmax(most, __shfl_xor(most, apart));
   return most;
 }
 template <typename T, int L>
-__device__ __forceinline__ bool line_finite(const T (&v)[32]) {
+__device__ __forceinline__ bool line_finite(const T (&v)[16]) {
   int bad = 0;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) bad |= !(fabs(v[i]) < T(__builtin_huge_valf()));
+  for (int i = 0; i < 16; ++i) bad |= !(fabs(v[i]) < T(__builtin_huge_valf()));
 #pragma unroll
   for (int apart = 1; apart < L; apart <<= 1) bad |= __shfl_xor(bad, apart);
   return !bad;
@@ -109,10 +109,10 @@ struct AppendCall {
   int32_t wide;
 };
 
-// L = D / 32 lanes to a line; a wave's indices go through LDS, where a lane's coefficients, L apart, become 32 neighbouring bytes.
+// L = D / 16 lanes to a line; a wave's indices go through LDS, where a lane's coefficients, L apart, become 16 neighbouring bytes.
 template <int kTf, int D>
 __global__ __launch_bounds__(256) void k_append(const AppendCall a) {
-  constexpr int L = D / 32, kLines = 64 / L, kPitch = D + 4;      // the pitch keeps lines L apart off one bank
+  constexpr int L = D / 16, kLines = 64 / L, kPitch = D + 4;      // the pitch keeps lines off one bank
   __shared__ uint32_t staged[4][kLines * kPitch / 4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane % L, in_wave = lane / L;
   const int64_t asked = (int64_t(blockIdx.x) * 4 + wave) * kLines + in_wave;
@@ -124,15 +124,15 @@ __global__ __launch_bounds__(256) void k_append(const AppendCall a) {
   const int64_t token = pair >> 1;
   const bool values = pair & 1;
   const pbz_lines& x = a.x[values];
-  double v[32];
-  load_run(x.data, a.type, token * x.token_stride + head * x.head_stride + part * 32, a.wide != 0, v);
+  double v[16];
+  load_run(x.data, a.type, token * x.token_stride + head * x.head_stride + part * 16, a.wide != 0, v);
   const int64_t slot = a.slots[token];
   const bool finite = line_finite<double, L>(v);
-  line::forward<kTf, double, L>(v, part);
+  line::forward<kTf, double, L>(v, lane);
   const double N = line_max<double, L>(v);
   uint8_t* bytes = reinterpret_cast<uint8_t*>(staged[wave]) + in_wave * kPitch;
 #pragma unroll
-  for (int k = 0; k < 32; ++k) {
+  for (int k = 0; k < 16; ++k) {
     const int index = N > 0.0 && finite ? int(rint(127.0 * v[k] / N)) : 0;
     bytes[line::coefficient<kTf, L>(part, k)] = uint8_t(index);
   }
@@ -140,10 +140,9 @@ __global__ __launch_bounds__(256) void k_append(const AppendCall a) {
   const int64_t page = slot >> a.cache.page_shift;
   if (!there || slot < 0 || page >= a.cache.n_pages) return;
   const int64_t to = (page * heads + head) * a.cache.page_size + (slot & (a.cache.page_size - 1));
-  const uint32_t* from = staged[wave] + (in_wave * kPitch + part * 32) / 4;
-  uint4* F = reinterpret_cast<uint4*>(const_cast<int8_t*>(values ? a.cache.v_F : a.cache.k_F) + to * D + part * 32);
-  F[0] = make_uint4(from[0], from[1], from[2], from[3]);
-  F[1] = make_uint4(from[4], from[5], from[6], from[7]);
+  const uint32_t* from = staged[wave] + (in_wave * kPitch + part * 16) / 4;
+  *reinterpret_cast<uint4*>(const_cast<int8_t*>(values ? a.cache.v_F : a.cache.k_F) + to * D + part * 16) =
+      make_uint4(from[0], from[1], from[2], from[3]);
   if (part == 0)
     store_float(const_cast<void*>(values ? a.cache.v_N : a.cache.k_N), a.cache.n_type, to, finite ? N : __builtin_nan(""));
 }
@@ -201,23 +200,23 @@ struct QueryCall {
 // Transformed, and held relative to the row's largest coefficient in 16 bits, +-32639 = 127 * 256 + 127, high and low byte signed.
 template <int kTf, int D>
 __global__ __launch_bounds__(256) void k_queries(const QueryCall a) {
-  constexpr int L = D / 32, kLines = 64 / L, kPitch = 2 * D + 4;
+  constexpr int L = D / 16, kLines = 64 / L, kPitch = 2 * D + 4;
   __shared__ uint32_t staged[4][kLines * kPitch / 4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane % L, in_wave = lane / L;
   const int64_t asked = (int64_t(blockIdx.x) * 4 + wave) * kLines + in_wave;
   const bool there = asked < a.rows;
   const int64_t row = there ? asked : a.rows - 1;
   const int64_t token = row / a.q_heads;
-  float v[32];
-  load_run(a.q, a.type, token * a.token_stride + (row - token * a.q_heads) * a.head_stride + part * 32, a.wide != 0, v);
+  float v[16];
+  load_run(a.q, a.type, token * a.token_stride + (row - token * a.q_heads) * a.head_stride + part * 16, a.wide != 0, v);
   const bool finite = line_finite<float, L>(v);
-  line::forward<kTf, float, L>(v, part);
+  line::forward<kTf, float, L>(v, lane);
   const float most = line_max<float, L>(v);
   const float up = finite && most > 0.f ? 32639.f / most : 0.f;
   const float sign = a.scale < 0.f ? -1.f : 1.f;
   uint8_t* bytes = reinterpret_cast<uint8_t*>(staged[wave]) + in_wave * kPitch;
 #pragma unroll
-  for (int k = 0; k < 32; ++k) {
+  for (int k = 0; k < 16; ++k) {
     const int index = up < __builtin_huge_valf() ? int(rintf(fminf(fmaxf(v[k] * up, -32639.f), 32639.f) * sign)) : 0;
     const int high = (index + 128) >> 8;
     const int at = line::coefficient<kTf, L>(part, k);
@@ -226,10 +225,10 @@ __global__ __launch_bounds__(256) void k_queries(const QueryCall a) {
   }
   wave_lds_sync();
   if (!there) return;
-  const uint32_t* from = staged[wave] + (in_wave * kPitch + part * 64) / 4;
-  uint4* q = reinterpret_cast<uint4*>(a.space.q + row * (2 * D) + part * 64);
+  const uint32_t* from = staged[wave] + (in_wave * kPitch + part * 32) / 4;
+  uint4* q = reinterpret_cast<uint4*>(a.space.q + row * (2 * D) + part * 32);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) q[i] = make_uint4(from[4 * i], from[4 * i + 1], from[4 * i + 2], from[4 * i + 3]);
+  for (int i = 0; i < 2; ++i) q[i] = make_uint4(from[4 * i], from[4 * i + 1], from[4 * i + 2], from[4 * i + 3]);
   if (part == 0) a.space.q_scale[row] = finite ? most * (1.f / 32639.f) * fabsf(a.scale) : __builtin_nanf("");
 }
 
@@ -247,94 +246,100 @@ struct FinishCall {
   int32_t n_splits;
 };
 
-// Joins the splits of a row, divides by the sum and transforms back.  kRows rows to a workgroup: 256 / L where there is one split, else
-// one, whose splits the threads share.
-template <int kTf, int D, bool kJoin>
+// Joins the splits of a row, divides by the sum and transforms back.  kRows rows to a workgroup: with one, the threads share its splits;
+// with more, every thread takes four columns of a row through all of them.
+template <int kTf, int D, int kRows>
 __global__ __launch_bounds__(256) void k_finish(const FinishCall a) {
-  constexpr int L = D / 32, kRows = kJoin ? 1 : 256 / L, kColumns = D / 4, kPitch = D + 4;
-  constexpr int kGroups = kJoin ? 256 / kColumns : 1;
-  __shared__ float staged[kRows * kGroups * kPitch];
-  __shared__ float weight[kMaxSplits];
+  constexpr int L = D / 16, kColumns = D / 4, kPitch = D + 4, kGroups = kRows == 1 ? 256 / kColumns : 1;
+  constexpr float kNone = -__builtin_huge_valf();
+  __shared__ alignas(16) float staged[kRows * kGroups * kPitch];
+  __shared__ float weight[kRows == 1 ? kMaxSplits : 1];
   __shared__ float joined[8];
   const int64_t first = int64_t(blockIdx.x) * kRows;
   const int tid = threadIdx.x;
-  if constexpr (kJoin) {
-    const int64_t row = first;
-    float2 state = make_float2(-__builtin_huge_valf(), 0.f);
-    if (tid < a.n_splits) state = a.space.state[int64_t(tid) * a.rows + row];
+  if constexpr (kRows == 1) {
+    float2 state = make_float2(kNone, 0.f);
+    if (tid < a.n_splits) state = a.space.state[int64_t(tid) * a.rows + first];
     float most = state.x;
     for (int apart = 1; apart < 64; apart <<= 1) most = fmaxf(most, __shfl_xor(most, apart));
     if ((tid & 63) == 0) joined[tid >> 6] = most;
     __syncthreads();
     most = fmaxf(fmaxf(joined[0], joined[1]), fmaxf(joined[2], joined[3]));
-    const float w = state.x == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(state.x - most);
-    weight[tid] = state.x == -__builtin_huge_valf() ? -1.f : w;
-    float total = state.x == -__builtin_huge_valf() ? 0.f : w * state.y;
+    const float w = state.x == kNone ? 0.f : __builtin_amdgcn_exp2f(state.x - most);
+    weight[tid] = state.x == kNone ? -1.f : w;           // (its sums have not been written)
+    float total = state.x == kNone ? 0.f : w * state.y;
     for (int apart = 1; apart < 64; apart <<= 1) total += __shfl_xor(total, apart);
     if ((tid & 63) == 0) joined[4 + (tid >> 6)] = total;
     __syncthreads();
     total = (joined[4] + joined[5]) + (joined[6] + joined[7]);
     const int column = tid % kColumns, group = tid / kColumns;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
     for (int s = group; s < a.n_splits; s += kGroups) {
       const float f = weight[s];
-      if (f < 0.f) continue;
-      const float4 u = *reinterpret_cast<const float4*>(a.space.sums + (int64_t(s) * a.rows + row) * D + column * 4);
-      sum.x += f * u.x;
-      sum.y += f * u.y;
-      sum.z += f * u.z;
-      sum.w += f * u.w;
+      const float4 u = *reinterpret_cast<const float4*>(a.space.sums + (int64_t(s) * a.rows + first) * D + column * 4);
+      sum.x += f < 0.f ? 0.f : f * u.x;
+      sum.y += f < 0.f ? 0.f : f * u.y;
+      sum.z += f < 0.f ? 0.f : f * u.z;
+      sum.w += f < 0.f ? 0.f : f * u.w;
     }
-    const float by = most == -__builtin_huge_valf() ? 0.f : 1.f / total;
-    float* to = staged + group * kPitch + column * 4;
-    to[0] = sum.x * by;
-    to[1] = sum.y * by;
-    to[2] = sum.z * by;
-    to[3] = sum.w * by;
+    const float by = most == kNone ? 0.f : 1.f / total;
+    *reinterpret_cast<float4*>(staged + group * kPitch + column * 4) = make_float4(sum.x * by, sum.y * by, sum.z * by, sum.w * by);
     __syncthreads();
     if (tid < D) {
       float s = 0.f;
       for (int g = 0; g < kGroups; ++g) s += staged[g * kPitch + tid];
       staged[tid] = s;                       // this thread's own column: nobody else reads it before the barrier
     }
-    if (tid == 0 && a.lse) a.lse[row] = (most + __builtin_amdgcn_logf(total)) * 0.693147180559945309f;
-    __syncthreads();
+    if (tid == 0 && a.lse) a.lse[first] = (most + __builtin_amdgcn_logf(total)) * 0.693147180559945309f;
   } else {
     for (int item = tid; item < kRows * kColumns; item += 256) {
       const int64_t row = first + item / kColumns;
-      float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
+      const int column = item % kColumns;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
       if (row < a.rows) {
-        const float2 state = a.space.state[row];
-        if (state.x != -__builtin_huge_valf()) {
-          const float by = 1.f / state.y;
-          u = *reinterpret_cast<const float4*>(a.space.sums + row * D + (item % kColumns) * 4);
-          u = make_float4(u.x * by, u.y * by, u.z * by, u.w * by);
+        float most = kNone, total = 0.f;
+#pragma unroll 4
+        for (int s = 0; s < a.n_splits; ++s) most = fmaxf(most, a.space.state[int64_t(s) * a.rows + row].x);
+#pragma unroll 4
+        for (int s = 0; s < a.n_splits; ++s) {
+          const float2 state = a.space.state[int64_t(s) * a.rows + row];
+          const float4 u = *reinterpret_cast<const float4*>(a.space.sums + (int64_t(s) * a.rows + row) * D + column * 4);
+          const bool none = state.x == kNone;            // (its sums have not been written)
+          const float f = none ? 0.f : __builtin_amdgcn_exp2f(state.x - most);
+          total += none ? 0.f : f * state.y;
+          sum.x += none ? 0.f : f * u.x;
+          sum.y += none ? 0.f : f * u.y;
+          sum.z += none ? 0.f : f * u.z;
+          sum.w += none ? 0.f : f * u.w;
         }
-        if (item % kColumns == 0 && a.lse) a.lse[row] = (state.x + __builtin_amdgcn_logf(state.y)) * 0.693147180559945309f;
+        const float by = most == kNone ? 0.f : 1.f / total;
+        sum = make_float4(sum.x * by, sum.y * by, sum.z * by, sum.w * by);
+        if (column == 0 && a.lse) a.lse[row] = (most + __builtin_amdgcn_logf(total)) * 0.693147180559945309f;
       }
-      *reinterpret_cast<float4*>(staged + (item / kColumns) * kPitch + (item % kColumns) * 4) = u;
+      *reinterpret_cast<float4*>(staged + (item / kColumns) * kPitch + column * 4) = sum;
     }
-    __syncthreads();
   }
-  if (tid >= kRows * L) return;              // whole lines: L divides
+  __syncthreads();
+  if (tid >= kRows * L) return;              // whole lines
   const int part = tid % L, in_block = tid / L;
   const int64_t row = first + in_block;
   const int64_t token = row / a.q_heads;
   const int64_t head = row - token * a.q_heads;
-  float v[32];
+  float v[16];
 #pragma unroll
-  for (int k = 0; k < 32; ++k) v[k] = staged[in_block * kPitch + line::coefficient<kTf, L>(part, k)];
-  line::inverse<kTf, float, L>(v, part);
+  for (int k = 0; k < 16; ++k) v[k] = staged[in_block * kPitch + line::coefficient<kTf, L>(part, k)];
+  line::inverse<kTf, float, L>(v, tid & 63);
   if (row >= a.rows) return;
   if (a.starts && (token < a.starts[0] || token >= a.starts[a.n_seqs])) {      // a row of no sequence
 #pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] = 0.f;
-    if (part == 0 && a.lse) a.lse[row] = -__builtin_huge_valf();
+    for (int k = 0; k < 16; ++k) v[k] = 0.f;
+    if (part == 0 && a.lse) a.lse[row] = kNone;
   }
-  uint16_t* out = static_cast<uint16_t*>(a.out) + token * a.token_stride + head * a.head_stride + part * 32;
-  uint32_t w[16];
+  uint16_t* out = static_cast<uint16_t*>(a.out) + token * a.token_stride + head * a.head_stride + part * 16;
+  uint32_t w[8];
 #pragma unroll
-  for (int k = 0; k < 16; ++k) {
+  for (int k = 0; k < 8; ++k) {
     uint16_t x, y;
     if (a.type == PBZ_BF16) {
       x = float_to_bf16_bits(v[2 * k]);
@@ -347,10 +352,10 @@ __global__ __launch_bounds__(256) void k_finish(const FinishCall a) {
   }
   if (a.wide) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(out)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    for (int i = 0; i < 2; ++i) reinterpret_cast<uint4*>(out)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
   } else {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
+    for (int k = 0; k < 8; ++k) {
       out[2 * k] = uint16_t(w[k]);
       out[2 * k + 1] = uint16_t(w[k] >> 16);
     }
@@ -414,6 +419,8 @@ struct AttendPlan {
   int waves_rows;
   int64_t row_blocks, split_blocks;
   int64_t n_splits, chunk;
+  int64_t records;         // splits as they are left to be joined
+  int finish_rows;         // rows to a workgroup there
   size_t q_bytes, scale_bytes, state_bytes, sum_bytes;
   size_t total() const { return q_bytes + scale_bytes + state_bytes + sum_bytes; }
 };
@@ -440,21 +447,25 @@ int plan_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_attention*
   int64_t length = a->max_pages * cache->page_size;
   if (a->max_length > 0) length = std::min(length, a->max_length);
   if (a->window > 0) length = std::min(length, a->window + fresh + 63);
-  // splits of the positions, where rows alone do not fill the chip; a split shorter than 128 would not pay for its record
+  // splits of the positions, where rows alone do not fill the chip
   const int64_t alone = a->n_seqs * cache->heads * tiles;
   int64_t splits = alone >= kComputeWaves ? 1 : (kComputeWaves + alone - 1) / alone;
-  splits = std::max<int64_t>(1, std::min<int64_t>({splits, kMaxSplits, length / 128}));
+  const int waves_rows = tiles >= 4 ? 4 : tiles >= 2 ? 2 : 1;
+  splits = std::max<int64_t>(1, std::min<int64_t>({splits, kMaxSplits * (4 / waves_rows), length / 128}));
   p->chunk = ((length + splits - 1) / splits + 63) / 64 * 64;
   p->n_splits = (length + p->chunk - 1) / p->chunk;
-  p->waves_rows = p->n_splits == 1 || tiles >= 4 ? 4 : tiles >= 2 ? 2 : 1;
+  p->waves_rows = p->n_splits == 1 ? 4 : waves_rows;
   const int waves_splits = 4 / p->waves_rows;
   p->row_blocks = (tiles + p->waves_rows - 1) / p->waves_rows;
   p->split_blocks = (p->n_splits + waves_splits - 1) / waves_splits;
+  p->records = p->split_blocks;
+  const int wave_rows = 64 / (c->vol / 16);
+  p->finish_rows = p->records > 16 && p->rows < 4096 ? 1 : p->rows < 16384 ? wave_rows : 4 * wave_rows;
   if (p->row_blocks > INT32_MAX / (a->n_seqs * cache->heads) / p->split_blocks) return PBZ_ERR_SHAPE;
   p->q_bytes = padded(uint64_t(p->rows) * 2 * c->vol);
   p->scale_bytes = padded(uint64_t(p->rows) * sizeof(float));
-  p->state_bytes = padded(uint64_t(p->rows) * p->n_splits * sizeof(float2));
-  p->sum_bytes = padded(uint64_t(p->rows) * p->n_splits * c->vol * sizeof(float));
+  p->state_bytes = padded(uint64_t(p->rows) * p->records * sizeof(float2));
+  p->sum_bytes = padded(uint64_t(p->rows) * p->records * c->vol * sizeof(float));
   return PBZ_OK;
 }
 
@@ -495,7 +506,7 @@ int pbz_cache_append(const pbz_codec* c, const pbz_cache* cache, int64_t n_token
   call.lines = n_tokens * 2 * cache->heads;
   call.type = type;
   c->used.store(true);
-  const int64_t lines = 256 / (c->vol / 32);
+  const int64_t lines = 256 / (c->vol / 16);
   const dim3 grid(unsigned((call.lines + lines - 1) / lines));
   for_line(c->transform, c->vol, [&](auto tf, auto dim) {
     k_append<decltype(tf)::value, decltype(dim)::value><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(call);
@@ -580,7 +591,7 @@ int pbz_cache_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_atten
   space.sums = reinterpret_cast<float*>(at += p.state_bytes);
   c->used.store(true);
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const int L = c->vol / 32;
+  const int L = c->vol / 16;
 
   QueryCall query;
   query.q = a->q;
@@ -631,11 +642,13 @@ int pbz_cache_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_atten
   finish.q_heads = a->q_heads;
   finish.type = a->type;
   finish.wide = aligned(a->out) && a->out_token_stride % 8 == 0 && a->out_head_stride % 8 == 0;
-  finish.n_splits = int32_t(p.n_splits);
+  finish.n_splits = int32_t(p.records);
   for_line(c->transform, c->vol, [&](auto tf, auto dim) {
-    constexpr int kTf = decltype(tf)::value, D = decltype(dim)::value;
-    if (p.n_splits > 1) k_finish<kTf, D, true><<<dim3(unsigned(p.rows)), 256, 0, s>>>(finish);
-    else k_finish<kTf, D, false><<<dim3(unsigned((p.rows + 256 / L - 1) / (256 / L))), 256, 0, s>>>(finish);
+    constexpr int kTf = decltype(tf)::value, D = decltype(dim)::value, kWave = 64 / (D / 16), kBlock = 4 * kWave;
+    const auto blocks = [&](int rows) { return dim3(unsigned((p.rows + rows - 1) / rows)); };
+    if (p.finish_rows == 1) k_finish<kTf, D, 1><<<blocks(1), 256, 0, s>>>(finish);
+    else if (p.finish_rows == kWave) k_finish<kTf, D, kWave><<<blocks(kWave), 256, 0, s>>>(finish);
+    else k_finish<kTf, D, kBlock><<<blocks(kBlock), 256, 0, s>>>(finish);
   });
   return hip_status(hipGetLastError());
 }
