@@ -13,7 +13,7 @@ namespace {
 
 constexpr int kMaxSplits = 256;
 constexpr int64_t kComputeWaves = 2048;      // waves that keep the chip busy: two to a SIMD
-constexpr int kPairsPerLaunch = 256;
+constexpr int kPairsPerLaunch = 448;          // 3.5 KiB of a launch's 4 KiB of arguments
 
 // 16 neighbouring elements as T; `wide`: the address is a multiple of 16 bytes
 template <typename T>
@@ -130,12 +130,23 @@ __global__ __launch_bounds__(256) void k_append(const AppendCall a) {
   const bool finite = line_finite<double, L>(v);
   line::forward<kTf, double, L>(v, lane);
   const double N = line_max<double, L>(v);
-  uint8_t* bytes = reinterpret_cast<uint8_t*>(staged[wave]) + in_wave * kPitch;
+  // Quotients as products with a reciprocal, off by some 2^-45 at most; next to a border between two indices the quotient itself decides.
+  const double reciprocal = N > 0.0 && finite ? 127.0 / N : 0.0;
+  double r[16];
+  bool close = false;
 #pragma unroll
   for (int k = 0; k < 16; ++k) {
-    const int index = N > 0.0 && finite ? int(rint(127.0 * v[k] / N)) : 0;
-    bytes[line::coefficient<kTf, L>(part, k)] = uint8_t(index);
+    const double q = v[k] * reciprocal;
+    r[k] = rint(q);
+    close = close || fabs(q - r[k]) > 0.5 - 0x1p-30;
   }
+  if (close) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) r[k] = reciprocal > 0.0 ? rint(127.0 * v[k] / N) : 0.0;
+  }
+  uint8_t* bytes = reinterpret_cast<uint8_t*>(staged[wave]) + in_wave * kPitch;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) bytes[line::coefficient<kTf, L>(part, k)] = uint8_t(int(r[k]));
   wave_lds_sync();
   const int64_t page = slot >> a.cache.page_shift;
   if (!there || slot < 0 || page >= a.cache.n_pages) return;
@@ -149,39 +160,36 @@ __global__ __launch_bounds__(256) void k_append(const AppendCall a) {
 
 // ---- copies of pages ---------------------------------------------------------------------------------------------------
 
+constexpr int kPiece = 16384;      // bytes of a page's part to a workgroup
+
 struct CopyCall {
-  void* pool[4];
-  int64_t page_bytes[4];       // multiples of 16
-  int64_t page_total;
+  char* pool[4];
+  int64_t bytes[4];            // of a page's part; a multiple of 16
+  int32_t pieces[4];           // of a page, up to and with this part
   int32_t pairs[2 * kPairsPerLaunch];
 };
 
-// a workgroup has 16 KiB of a page's four parts, laid end to end
+// The pairs travel with the launch: no copy to the device, nothing to keep alive, and a captured graph holds them.
 __global__ __launch_bounds__(256) void k_copy_pages(const CopyCall a) {
   const int64_t from = a.pairs[2 * blockIdx.y], to = a.pairs[2 * blockIdx.y + 1];
-  uint4 held[4];
-  char* where[4];
+  const int x = int(blockIdx.x);
+  const int part = (x >= a.pieces[0]) + (x >= a.pieces[1]) + (x >= a.pieces[2]);
+  char* const pool = part == 0 ? a.pool[0] : part == 1 ? a.pool[1] : part == 2 ? a.pool[2] : a.pool[3];
+  const int64_t bytes = part == 0 ? a.bytes[0] : part == 1 ? a.bytes[1] : part == 2 ? a.bytes[2] : a.bytes[3];
+  const int before = part == 0 ? 0 : part == 1 ? a.pieces[0] : part == 2 ? a.pieces[1] : a.pieces[2];
+  const int64_t at = int64_t(x - before) * kPiece;
+  const uint4* const source = reinterpret_cast<const uint4*>(pool + from * bytes + at);
+  uint4* const target = reinterpret_cast<uint4*>(pool + to * bytes + at);
+  const int count = int((bytes - at < kPiece ? bytes - at : kPiece) / 16);
+  if (count == kPiece / 16) {
+    uint4 held[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    int64_t at = (int64_t(blockIdx.x) * 1024 + i * 256 + threadIdx.x) * 16;
-    char* pool = nullptr;
-    int64_t size = 0;
-    if (at < a.page_total) {
+    for (int i = 0; i < 4; ++i) held[i] = source[i * 256 + threadIdx.x];
 #pragma unroll
-      for (int part = 0; part < 4; ++part) {
-        if (!pool && at < a.page_bytes[part]) {
-          pool = static_cast<char*>(a.pool[part]) + at;
-          size = a.page_bytes[part];
-        }
-        at -= a.page_bytes[part];
-      }
-    }
-    where[i] = pool ? pool + to * size : nullptr;
-    if (pool) held[i] = *reinterpret_cast<const uint4*>(pool + from * size);
+    for (int i = 0; i < 4; ++i) target[i * 256 + threadIdx.x] = held[i];
+  } else {
+    for (int i = threadIdx.x; i < count; i += 256) target[i] = source[i];
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (where[i]) *reinterpret_cast<uint4*>(where[i]) = held[i];
 }
 
 // ---- attention: queries before, results after ----------------------------------------------------------------------------
@@ -543,17 +551,17 @@ int pbz_cache_copy_pages(const pbz_codec* c, const pbz_cache* cache, int64_t n_p
   CopyCall call;
   const int64_t lines = int64_t(cache->heads) * cache->page_size;
   void* const pools[4] = {cache->k_F, cache->v_F, cache->k_N, cache->v_N};
-  call.page_total = 0;
+  int64_t pieces = 0;
   for (int i = 0; i < 4; ++i) {
-    call.pool[i] = pools[i];
-    call.page_bytes[i] = lines * (i < 2 ? c->vol : ftype_bytes(c->ftype));
-    call.page_total += call.page_bytes[i];
+    call.pool[i] = static_cast<char*>(pools[i]);
+    call.bytes[i] = lines * (i < 2 ? c->vol : ftype_bytes(c->ftype));
+    pieces += (call.bytes[i] + kPiece - 1) / kPiece;
+    call.pieces[i] = int32_t(pieces);
   }
-  const unsigned parts = unsigned((call.page_total + 16383) / 16384);
   for (int64_t at = 0; at < n_pairs; at += kPairsPerLaunch) {
     const int64_t n = std::min<int64_t>(kPairsPerLaunch, n_pairs - at);
     std::copy(pairs + 2 * at, pairs + 2 * (at + n), call.pairs);
-    k_copy_pages<<<dim3(parts, unsigned(n)), 256, 0, static_cast<hipStream_t>(stream)>>>(call);
+    k_copy_pages<<<dim3(unsigned(pieces), unsigned(n)), 256, 0, static_cast<hipStream_t>(stream)>>>(call);
     const int launched = hip_status(hipGetLastError());
     if (launched != PBZ_OK) return launched;
   }
