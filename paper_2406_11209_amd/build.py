@@ -22,7 +22,8 @@ SOURCES = ["pbz_api.hip", "pbz_generic.hip", "pbz_ops.hip", "pbz_ops_staged.hip"
            "pbz_fast_oct8.hip", "pbz_fast_cube16.hip", "pbz_wasserstein.hip", "pbz_tiled.hip", "pbz_lines.hip", "pbz_brick.hip", "pbz_brick_lines.hip", "pbz_brick_small.hip",
            "pbz_brick_flat.hip", "pbz_brick_wide.hip", "pbz_brick_planes.hip", "pbz_brick_cubes.hip", "pbz_brick_tesseracts.hip",
            "pbz_brick_long_tesseracts.hip", "pbz_static.hip", "pbz_copy.hip",
-           "pbz_cache.hip", "pbz_attend.hip", "pbz_pages.hip"]
+           "pbz_cache.hip", "pbz_attend_32.hip", "pbz_attend_64.hip", "pbz_attend_128.hip", "pbz_attend_256.hip",
+           "pbz_pages.hip"]
 
 # Packed-FP32 code generation is switched off on purpose (the flag applies to the device pass; the host
 # pass prints a harmless "unknown feature" warning).

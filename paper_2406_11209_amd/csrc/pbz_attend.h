@@ -13,8 +13,9 @@
 //            have the same); the largest is 2^15, and what is 2^-29 of it is still a normal FP16 number.  V's bytes become FP16 integers
 //            by permutes: 0x6400 | (F + 128) is 1024 + 128 + F, minus 1152.
 // Lanes 16 apart share a position's line: a line of 128 is one 128-byte read of 8 (keys) or 16 lanes (values).
-#include "pbz_cache_internal.h"
-#include "pbz_device.h"
+#pragma once
+
+#include "pbz_cache_lines.h"
 
 namespace pbz {
 namespace {
@@ -496,13 +497,65 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
   }
 }
 
+// The lane, of which the compiler must not know that it is the same every time: what is derived from it before and after the pass over the
+// positions would otherwise be kept in registers during it, where there are none to spare.
+__device__ __forceinline__ int this_lane() {
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+
+// Results of 16 rows, first ..: a wave's coefficients, from LDS, transformed back and written.
+template <int D>
+constexpr int kResultPitch = D + 4;
+template <int D>
+__device__ __forceinline__ void write_results(const AttendCall& a, const Part& part, uint32_t first, const float* staged) {
+  constexpr int L = D / 16, kLines = 64 / L < 16 ? 64 / L : 16;
+  const int lane = this_lane(), in_line = lane % L;
+  const uint32_t groups = uint32_t(a.groups);
+#pragma unroll 1
+  for (int base = 0; base < 16 && first + base < part.rows; base += kLines) {
+    const int line = base + lane / L < 16 ? base + lane / L : 15;
+    float v[16];
+    if (a.transform == PBZ_TRANSFORM_HAAR) {
+#pragma unroll
+      for (int k = 0; k < 16; ++k) v[k] = staged[line * kResultPitch<D> + line::coefficient<kTfHaar, L>(in_line, k)];
+      line::inverse<kTfHaar, float, L>(v, lane);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 16; ++k) v[k] = staged[line * kResultPitch<D> + line::coefficient<kTfDct, L>(in_line, k)];
+      line::inverse<kTfDct, float, L>(v, lane);
+    }
+    const uint32_t row = first + line, token = row / groups;
+    if (row < part.rows && base + lane / L < 16)
+      store_run(static_cast<uint16_t*>(a.out) + (part.first + token) * a.out_token_stride +
+                    (int64_t(part.head) * groups + (row - token * groups)) * a.out_head_stride + in_line * 16, a.type, a.out_wide != 0, v);
+  }
+}
+
+// Rows of no sequence, before the first and behind the last, are zero: the first and the last sequence's workgroups see to them.
+__device__ __forceinline__ void zero_rest(const AttendCall& a, const Part& part, int dim) {
+  if (!a.starts || part.row_block != 0 || part.record != 0) return;
+  for (int side = 0; side < 2; ++side) {
+    if (part.seq != (side ? a.n_seqs - 1 : 0)) continue;
+    int64_t from = side ? a.starts[a.n_seqs] : 0, to = side ? a.n_tokens : a.starts[0];
+    from = from < 0 ? 0 : from;
+    to = to > a.n_tokens ? a.n_tokens : to;
+    for (int64_t token = from; token < to; ++token)
+      for (int i = threadIdx.x; i < a.groups * dim; i += 256) {
+        const int64_t head = int64_t(part.head) * a.groups + i / dim;
+        static_cast<uint16_t*>(a.out)[token * a.out_token_stride + head * a.out_head_stride + i % dim] = 0;
+        if (a.lse && i % dim == 0) a.lse[token * a.q_heads + head] = kNegInf;
+      }
+  }
+}
+
 // A wave's 32 rows of one head in tiles of 32: the same as Rows, a lane having one row and 16 of a step's 32 positions,
 // 8 (i / 4) + 4 half + i % 4.  Whether the weights' reference has to grow shows in their sum, which is taken anyway: a lane's part of it
 // may reach 2^8, and is infinite or no number while there is no reference.
 template <int D, bool kFine>
 struct TallRows {
   static constexpr int KS = D / 32, DT = D / 32;
-  int64_t place;
   int low, high;
   i32x4 q_high[KS], q_low[KS];
   float q_scale, minus_top, total, widest;
@@ -516,7 +569,6 @@ struct TallRows {
     const uint32_t row = there ? asked : part.rows - 1;
     const uint32_t token = row / groups;
     const int64_t at = (part.first + token) * a.q_heads + int64_t(part.head) * a.groups + (row - token * groups);
-    place = there ? at : -1;
     const int position = part.length - part.fresh + int(token);
     high = !there ? -1 : a.causal ? position : part.length - 1;
     low = a.window > 0 && position - int(a.window) + 1 > 0 ? position - int(a.window) + 1 : 0;
@@ -623,13 +675,35 @@ struct TallRows {
     if constexpr (kFine) sum[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p_low[b], sum[t], 0, 0, 0);
   }
 
-  // a lane has coefficients (8 (i / 4) + 4 half + i % 4) DT + t of its row
-  __device__ __forceinline__ void store(const AttendCall& a, int record, int half) {
+  // A lane has coefficients (8 (i / 4) + 4 half + i % 4) DT + t of its row: a record, or where there are no splits the result, by way of the
+  // wave's room in LDS.
+  __device__ __forceinline__ void store(const AttendCall& a, const Part& part, uint32_t first_row, float* staged, int c, int half) {
     const float l = total + __shfl_xor(total, 32);
-    if (place < 0) return;
     const float top = l != l ? 0.f : -minus_top;         // a row that sees a NaN is one, also where it sees nothing else
     const float unit = widest * (1.f / (128.f * 127.f));
-    const int64_t to = int64_t(record) * a.n_tokens * a.q_heads + place;
+    const bool there = first_row + c < part.rows;
+    const uint32_t row = there ? first_row + c : part.rows - 1, token = row / uint32_t(a.groups);
+    const int64_t place = (part.first + token) * a.q_heads + int64_t(part.head) * a.groups + (row - token * uint32_t(a.groups));
+    if (a.records == 1) {
+      if (a.lse && half == 0 && there) a.lse[place] = (top + __builtin_amdgcn_logf(l)) * 0.693147180559945309f;
+      const float by = top == kNegInf ? 0.f : unit / l;
+#pragma unroll 1
+      for (int pass = 0; pass < 2; ++pass) {
+        if (c / 16 == pass) {
+          float* to = staged + c % 16 * kResultPitch<D> + half * 4 * DT;
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int t = 0; t < DT; ++t) to[(8 * (i / 4) + i % 4) * DT + t] = sum[t][i] * by;
+        }
+        wave_lds_sync();
+        write_results<D>(a, part, first_row + pass * 16, staged);
+        wave_lds_sync();
+      }
+      return;
+    }
+    if (!there) return;
+    const int64_t to = int64_t(part.record) * a.n_tokens * a.q_heads + place;
     if (half == 0) a.space.state[to] = make_float2(top, l);
     if (top == kNegInf) return;
     float* out = a.space.sums + to * D + half * 4 * DT;
@@ -690,14 +764,22 @@ template <int D, bool kFine, int kN>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const AttendCall a) {
   constexpr int DT = D / 32, KS = D / 32, VW = D >= 128 ? D / 128 : 1;
   constexpr int kChunks = D / 16, kKeyLoads = D / 64;      // 16-byte pieces of a line; loads of 64 of them for a wave's 16 lines
-  __shared__ u32x4 operands[2][4][DT][64];
-  __shared__ i32x4 keys[3][64][kChunks];         // piece p of line l at p ^ (l >> s), so that a read of 32 lines has 8 lanes on every bank
+  // LDS: stages, and in the end the waves' rooms for their results
+  struct Stages {
+    u32x4 operands[2][4][DT][64];
+    i32x4 keys[3][64][kChunks];                  // piece p of line l at p ^ (l >> s), so that a read of 32 lines has 8 lanes on every bank
+  };
+  constexpr int kRoom = 16 * kResultPitch<D>;
+  __shared__ alignas(16) uint8_t memory[int(sizeof(Stages)) > 16 * kRoom ? int(sizeof(Stages)) : 16 * kRoom];
+  auto& operands = reinterpret_cast<Stages*>(memory)->operands;
+  auto& keys = reinterpret_cast<Stages*>(memory)->keys;
   __shared__ alignas(16) float scale_of[2][2][64];           // keys, values (over the largest so far, times 2^7)
   __shared__ float2 reach[2];                    // the largest N of values so far, up to the next power of two; not 0: some N is not finite
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, half = lane >> 5;
   Part part;
   if (!part.find(a, 0)) return;
+  if (a.records == 1) zero_rest(a, part, D);
   const uint32_t apart = a.row_blocks * 128;
   TallRows<D, kFine> rows;
   for (uint32_t first = part.row_block * 128; first < part.rows; first += apart) {
@@ -706,7 +788,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
     const int begin = start < all.to ? int(start) : all.to;
     const int end = part.split == a.n_splits - 1 || start + a.chunk > all.to ? all.to : int(start + a.chunk);
     const uint32_t own = first + wave * 32;
-    rows.begin(a, part, own, c, half);
+    const int at_first = this_lane();
+    rows.begin(a, part, own, at_first & 31, at_first >> 5);
     const Range sees(a, part, own < part.rows ? own : first, own < part.rows ? (part.rows - own < 32 ? part.rows - own : 32) : 1);
     if (begin < end) {
       const int32_t* table = a.table + part.seq * a.table_stride;
@@ -853,47 +936,37 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
         __syncthreads();
       }
     }
-    rows.store(a, part.record, half);
+    const int at_end = this_lane();
+    rows.store(a, part, own, reinterpret_cast<float*>(memory) + wave * kRoom, at_end & 31, at_end >> 5);
+    __syncthreads();
   }
 }
 
 template <int D, int kN>
-int launch(int rows, bool fine, const AttendCall& call, hipStream_t s) {
+int launch(bool tall, int rows, bool fine, const AttendCall& call, hipStream_t s) {
   const dim3 grid((call.blocks + 7) / 8 * 8), block(256);
-  if (rows == 16) {
+  if (tall) {
+    if constexpr (D >= 64) {
+      if (fine) k_attend_tall<D, true, kN><<<grid, block, 0, s>>>(call);
+      else k_attend_tall<D, false, kN><<<grid, block, 0, s>>>(call);
+    }
+  } else if (rows == 16) {
     if (fine) k_attend<D, 1, true, kN><<<grid, block, 0, s>>>(call);
     else k_attend<D, 1, false, kN><<<grid, block, 0, s>>>(call);
   } else {
-    if constexpr (D >= 64) {
-      if (call.waves_rows == 4) {
-        if (fine) k_attend_tall<D, true, kN><<<grid, block, 0, s>>>(call);
-        else k_attend_tall<D, false, kN><<<grid, block, 0, s>>>(call);
-        return hip_status(hipGetLastError());
-      }
-    }
     if (fine) k_attend<D, 2, true, kN><<<grid, block, 0, s>>>(call);
     else k_attend<D, 2, false, kN><<<grid, block, 0, s>>>(call);
   }
   return hip_status(hipGetLastError());
 }
 template <int D>
-int launch(int rows, bool fine, const AttendCall& call, hipStream_t s) {
+int launch(bool tall, int rows, bool fine, const AttendCall& call, hipStream_t s) {
   switch (call.cache.n_type) {
-    case PBZ_F32: return launch<D, PBZ_F32>(rows, fine, call, s);
-    case PBZ_BF16: return launch<D, PBZ_BF16>(rows, fine, call, s);
-    default: return launch<D, PBZ_F16>(rows, fine, call, s);
+    case PBZ_F32: return launch<D, PBZ_F32>(tall, rows, fine, call, s);
+    case PBZ_BF16: return launch<D, PBZ_BF16>(tall, rows, fine, call, s);
+    default: return launch<D, PBZ_F16>(tall, rows, fine, call, s);
   }
 }
 
 }  // namespace
-
-int launch_attend(int dim, int rows, bool fine, const AttendCall& call, hipStream_t s) {
-  switch (dim) {
-    case 32: return launch<32>(rows, fine, call, s);
-    case 64: return launch<64>(rows, fine, call, s);
-    case 128: return launch<128>(rows, fine, call, s);
-    default: return launch<256>(rows, fine, call, s);
-  }
-}
-
 }  // namespace pbz

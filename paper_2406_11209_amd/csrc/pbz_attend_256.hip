@@ -1,0 +1,6 @@
+// Attention over a cache of lines of 256: see pbz_attend.h.
+#include "pbz_attend.h"
+
+int pbz::launch_attend_256(bool tall, int rows, bool fine, const AttendCall& call, hipStream_t s) {
+  return launch<256>(tall, rows, fine, call, s);
+}

@@ -4,9 +4,7 @@
 #include <cmath>
 #include <vector>
 
-#include "pbz_cache_internal.h"
-#include "pbz_device.h"
-#include "pbz_line_transform.h"
+#include "pbz_cache_lines.h"
 
 namespace pbz {
 namespace {
@@ -14,89 +12,6 @@ namespace {
 constexpr int kMaxSplits = 256;
 constexpr int64_t kComputeWaves = 2048;      // waves that keep the chip busy: two to a SIMD
 constexpr int kPairsPerLaunch = 448;          // 3.5 KiB of a launch's 4 KiB of arguments
-
-// 16 neighbouring elements as T; `wide`: the address is a multiple of 16 bytes
-template <typename T>
-__device__ __forceinline__ void load_run(const void* p, int type, int64_t at, bool wide, T (&v)[16]) {
-  if (type == PBZ_F64) {
-    const double* x = static_cast<const double*>(p) + at;
-    if (wide) {
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const double2 u = *reinterpret_cast<const double2*>(x + i);
-        v[i] = T(u.x);
-        v[i + 1] = T(u.y);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = T(x[i]);
-    }
-  } else if (type == PBZ_F32) {
-    const float* x = static_cast<const float*>(p) + at;
-    if (wide) {
-#pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        const float4 u = *reinterpret_cast<const float4*>(x + i);
-        v[i] = T(u.x);
-        v[i + 1] = T(u.y);
-        v[i + 2] = T(u.z);
-        v[i + 3] = T(u.w);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = T(x[i]);
-    }
-  } else {
-    const uint16_t* x = static_cast<const uint16_t*>(p) + at;
-    uint32_t w[8];
-    if (wide) {
-#pragma unroll
-      for (int i = 0; i < 8; i += 4) {
-        const uint4 u = *reinterpret_cast<const uint4*>(x + 2 * i);
-        w[i] = u.x;
-        w[i + 1] = u.y;
-        w[i + 2] = u.z;
-        w[i + 3] = u.w;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = uint32_t(x[2 * i]) | (uint32_t(x[2 * i + 1]) << 16);
-    }
-    if (type == PBZ_BF16) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[2 * i] = T(__uint_as_float(w[i] << 16));
-        v[2 * i + 1] = T(__uint_as_float(w[i] & 0xffff0000u));
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[2 * i] = T(float(__builtin_bit_cast(_Float16, uint16_t(w[i]))));
-        v[2 * i + 1] = T(float(__builtin_bit_cast(_Float16, uint16_t(w[i] >> 16))));
-      }
-    }
-  }
-}
-
-// the largest magnitude of a line, and whether all of its values are finite: the same in its L lanes
-template <typename T, int L>
-__device__ __forceinline__ T line_max(const T (&v)[16]) {
-  T most = T(0);
-#pragma unroll
-  for (int i = 0; i < 16; ++i) most = fmax(most, fabs(v[i]));
-#pragma unroll
-  for (int apart = 1; apart < L; apart <<= 1) most = fmax(most, __shfl_xor(most, apart));
-  return most;
-}
-template <typename T, int L>
-__device__ __forceinline__ bool line_finite(const T (&v)[16]) {
-  int bad = 0;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) bad |= !(fabs(v[i]) < T(__builtin_huge_valf()));
-#pragma unroll
-  for (int apart = 1; apart < L; apart <<= 1) bad |= __shfl_xor(bad, apart);
-  return !bad;
-}
 
 // ---- append ----------------------------------------------------------------------------------------------------------
 
@@ -344,30 +259,7 @@ __global__ __launch_bounds__(256) void k_finish(const FinishCall a) {
     for (int k = 0; k < 16; ++k) v[k] = 0.f;
     if (part == 0 && a.lse) a.lse[row] = kNone;
   }
-  uint16_t* out = static_cast<uint16_t*>(a.out) + token * a.token_stride + head * a.head_stride + part * 16;
-  uint32_t w[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    uint16_t x, y;
-    if (a.type == PBZ_BF16) {
-      x = float_to_bf16_bits(v[2 * k]);
-      y = float_to_bf16_bits(v[2 * k + 1]);
-    } else {
-      x = __builtin_bit_cast(uint16_t, _Float16(v[2 * k]));
-      y = __builtin_bit_cast(uint16_t, _Float16(v[2 * k + 1]));
-    }
-    w[k] = uint32_t(x) | (uint32_t(y) << 16);
-  }
-  if (a.wide) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) reinterpret_cast<uint4*>(out)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      out[2 * k] = uint16_t(w[k]);
-      out[2 * k + 1] = uint16_t(w[k] >> 16);
-    }
-  }
+  store_run(static_cast<uint16_t*>(a.out) + token * a.token_stride + head * a.head_stride + part * 16, a.type, a.wide != 0, v);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -429,6 +321,8 @@ struct AttendPlan {
   int64_t n_splits, chunk;
   int64_t records;         // splits as they are left to be joined
   int finish_rows;         // rows to a workgroup there
+  bool tall;               // the kernel for many rows, which finishes what is not split by itself
+  bool whole() const { return tall && records == 1; }
   size_t q_bytes, scale_bytes, state_bytes, sum_bytes;
   size_t total() const { return q_bytes + scale_bytes + state_bytes + sum_bytes; }
 };
@@ -467,13 +361,14 @@ int plan_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_attention*
   p->row_blocks = (tiles + p->waves_rows - 1) / p->waves_rows;
   p->split_blocks = (p->n_splits + waves_splits - 1) / waves_splits;
   p->records = p->split_blocks;
+  p->tall = c->vol >= 64 && p->tile == 32 && p->waves_rows == 4 && tiles >= 3;
   const int wave_rows = 64 / (c->vol / 16);
   p->finish_rows = p->records > 16 && p->rows < 4096 ? 1 : p->rows < 16384 ? wave_rows : 4 * wave_rows;
   if (p->row_blocks > INT32_MAX / (a->n_seqs * cache->heads) / p->split_blocks) return PBZ_ERR_SHAPE;
   p->q_bytes = padded(uint64_t(p->rows) * 2 * c->vol);
   p->scale_bytes = padded(uint64_t(p->rows) * sizeof(float));
-  p->state_bytes = padded(uint64_t(p->rows) * p->records * sizeof(float2));
-  p->sum_bytes = padded(uint64_t(p->rows) * p->records * c->vol * sizeof(float));
+  p->state_bytes = p->whole() ? 0 : padded(uint64_t(p->rows) * p->records * sizeof(float2));
+  p->sum_bytes = p->whole() ? 0 : padded(uint64_t(p->rows) * p->records * c->vol * sizeof(float));
   return PBZ_OK;
 }
 
@@ -618,6 +513,14 @@ int pbz_cache_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_atten
   st = hip_status(hipGetLastError());
   if (st != PBZ_OK) return st;
 
+  call.out = a->out;
+  call.lse = a->lse;
+  call.out_token_stride = a->out_token_stride;
+  call.out_head_stride = a->out_head_stride;
+  call.type = a->type;
+  call.transform = c->transform;
+  call.out_wide = aligned(a->out) && a->out_token_stride % 8 == 0 && a->out_head_stride % 8 == 0;
+  call.records = int32_t(p.records);
   call.starts = a->starts;
   call.lengths = a->lengths;
   call.table = a->table;
@@ -635,8 +538,8 @@ int pbz_cache_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_atten
   call.row_blocks = uint32_t(p.row_blocks);
   call.split_blocks = uint32_t(p.split_blocks);
   call.blocks = uint32_t(p.row_blocks * p.split_blocks * a->n_seqs * cache->heads);
-  st = launch_attend(c->vol, p.tile, a->type == PBZ_F16, call, s);
-  if (st != PBZ_OK) return st;
+  st = launch_attend(c->vol, p.tall, p.tile, a->type == PBZ_F16, call, s);
+  if (st != PBZ_OK || p.whole()) return st;
 
   FinishCall finish;
   finish.space = space;
@@ -649,7 +552,7 @@ int pbz_cache_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_atten
   finish.n_seqs = a->n_seqs;
   finish.q_heads = a->q_heads;
   finish.type = a->type;
-  finish.wide = aligned(a->out) && a->out_token_stride % 8 == 0 && a->out_head_stride % 8 == 0;
+  finish.wide = call.out_wide;
   finish.n_splits = int32_t(p.records);
   for_line(c->transform, c->vol, [&](auto tf, auto dim) {
     constexpr int kTf = decltype(tf)::value, D = decltype(dim)::value, kWave = 64 / (D / 16), kBlock = 4 * kWave;

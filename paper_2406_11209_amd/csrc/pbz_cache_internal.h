@@ -22,13 +22,18 @@ struct CacheGeom {
 struct AttendSpace {
   int8_t* q;               // [row][2][D]: a coefficient is (256 high + low) times the row's scale
   float* q_scale;          // [row], times scale log2(e) / 127
-  float2* state;           // [split][row]: running maximum (of scores in units of ln 2) and sum
-  float* sums;             // [split][row][D]: coefficients of the weighted sum; not written where the maximum is -infinity
+  float2* state;           // [record][row]: running maximum (of scores in units of ln 2) and sum
+  float* sums;             // [record][row][D]: coefficients of the weighted sum; not written where the maximum is -infinity
 };
 
 struct AttendCall {
   CacheGeom cache;
   AttendSpace space;
+  void* out;
+  float* lse;
+  int64_t out_token_stride, out_head_stride;
+  int32_t type, transform, out_wide;
+  int32_t records;         // splits that are left to be joined
   const int32_t* starts;
   const int32_t* lengths;
   const int32_t* table;
@@ -47,7 +52,18 @@ struct AttendCall {
   uint32_t blocks;
 };
 
-// rows: query rows to a wave, 16 or 32
-int launch_attend(int dim, int rows, bool fine, const AttendCall& call, hipStream_t s);
+// tall: the kernel for many rows; rows: query rows to a wave, 16 or 32; a translation unit per D
+int launch_attend_32(bool tall, int rows, bool fine, const AttendCall& call, hipStream_t s);
+int launch_attend_64(bool tall, int rows, bool fine, const AttendCall& call, hipStream_t s);
+int launch_attend_128(bool tall, int rows, bool fine, const AttendCall& call, hipStream_t s);
+int launch_attend_256(bool tall, int rows, bool fine, const AttendCall& call, hipStream_t s);
+inline int launch_attend(int dim, bool tall, int rows, bool fine, const AttendCall& call, hipStream_t s) {
+  switch (dim) {
+    case 32: return launch_attend_32(tall, rows, fine, call, s);
+    case 64: return launch_attend_64(tall, rows, fine, call, s);
+    case 128: return launch_attend_128(tall, rows, fine, call, s);
+    default: return launch_attend_256(tall, rows, fine, call, s);
+  }
+}
 
 }  // namespace pbz

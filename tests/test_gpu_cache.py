@@ -267,6 +267,72 @@ def test_attend(case):
         check_attend(cache, q, again, None, tables, lengths, counts, causal, window)
 
 
+# chunks of many rows, with and without splits of the positions: dim, heads, groups, page, array, work, transform, lengths, new, causal, window
+TALL = [
+    (128, 2, 4, 64, "bf16", "f32", "dct", [6000], [64], True, 0),
+    (128, 1, 8, 16, "f16", "bf16", "haar", [2500, 0, 70, 31], [40, 5, 70, 40], True, 0),
+    (64, 3, 2, 32, "bf16", "f16", "dct", [4100, 200], [77, 130], True, 300),
+    (64, 1, 16, 16, "f16", "f32", "haar", [3000], [9], False, 0),
+    (256, 1, 4, 64, "f16", "f16", "dct", [2000, 129], [33, 129], True, 0),
+    (256, 2, 2, 1024, "bf16", "f32", "haar", [900], [200], True, 64),
+    (32, 2, 8, 16, "bf16", "f32", "dct", [1500, 40], [60, 40], True, 0),
+    (128, 1, 5, 128, "bf16", "bf16", "dct", [1300], [300], True, 1),
+]
+
+
+@pytest.mark.parametrize("case", TALL, ids=[f"{i}" for i in range(len(TALL))])
+def test_attend_many_rows_with_holes(case):
+    """Pages outside the pool among the sequences', poison in everything that no row may see."""
+    dim, heads, groups, page, array, work, transform, lengths, counts, causal, window = case
+    n_pages = sum(-(-n // page) for n in lengths) + 2
+    cache = filled(PagedCache(dim, heads, n_pages, page, work, transform), 41)
+    tables, table, length_t = deal(cache, lengths, 42)
+    owned = torch.zeros(n_pages, page, dtype=torch.bool, device="cuda")
+    hidden = (n_pages, -3)
+    for b, (t, n) in enumerate(zip(tables, lengths)):
+        for i in range(len(t)):
+            if i % 5 == 2:
+                t[i] = hidden[i % 2]
+                table[b, i] = t[i]
+            else:
+                owned[t[i], :max(0, min(page, n - i * page))] = True
+    for N in (cache.k_N, cache.v_N):
+        N.masked_fill_(~owned[:, None, :], math.inf)
+    g = torch.Generator(device="cuda").manual_seed(43)
+    q = torch.randn(sum(counts), heads * groups, dim, generator=g, device="cuda").to(FLOATS[array])
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    for most, longest in ((max(counts), 0), (max(counts), 128), (1, 0)):
+        out = cache.attend(q, table, length_t, starts=starts_of(counts), max_new=most, max_length=longest, causal=causal,
+                           window=window, lse=lse)
+        check_attend(cache, q, out, lse, tables, lengths, counts, causal, window, hidden_pages=hidden)
+
+
+def test_rows_of_no_sequence_are_zero_beside_many_rows():
+    cache = filled(PagedCache(128, 2, 12, 64), 44)
+    tables, table, lengths = deal(cache, [200, 100], 45)
+    q = torch.randn(200, 8, 128, device="cuda").to(torch.bfloat16)
+    starts = torch.tensor([11, 111, 190], dtype=torch.int32, device="cuda")
+    out, lse = torch.full_like(q, 3.0), torch.full(q.shape[:2], 3.0, device="cuda")
+    cache.attend(q, table, lengths, starts=starts, max_new=100, out=out, lse=lse)
+    assert bool((out[:11] == 0).all()) and bool((out[190:] == 0).all())
+    assert bool((lse[:11] == -math.inf).all()) and bool((lse[190:] == -math.inf).all())
+    check_attend(cache, q[11:190], out[11:190], lse[11:190], tables, [200, 100], [100, 79])
+
+
+def test_values_that_widen_late():
+    """The largest N of the values at the end of a long sequence, tiny ones before."""
+    for dtype in (torch.bfloat16, torch.float16):
+        cache = filled(PagedCache(128, 1, 20, 64), 46, spread=False)
+        tables, table, lengths = deal(cache, [1200], 47)
+        for i, p in enumerate(tables[0]):
+            cache.v_N[p] *= 2.0 ** (i - 12)
+        q = torch.randn(100, 2, 128, device="cuda").to(dtype)
+        out = cache.attend(q, table, lengths, starts=starts_of([100]))
+        check_attend(cache, q, out, None, tables, [1200], [100])
+        one = cache.attend(q[-1:], table, lengths)
+        check_attend(cache, q[-1:], one, None, tables, [1200], [1])
+
+
 def test_attend_takes_any_alignment():
     cache = filled(PagedCache(64, 2, 12, 16), 11)
     tables, table, lengths = deal(cache, [40, 100], 12)
