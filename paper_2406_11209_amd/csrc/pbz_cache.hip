@@ -10,7 +10,7 @@ namespace pbz {
 namespace {
 
 constexpr int kMaxSplits = 256;
-constexpr int64_t kComputeWaves = 2048;      // waves that keep the chip busy: two to a SIMD
+constexpr int64_t kBusyWaves = 2048;         // waves that keep the chip busy: two to a SIMD
 constexpr int kPairsPerLaunch = 448;          // 3.5 KiB of a launch's 4 KiB of arguments
 
 // ---- append ----------------------------------------------------------------------------------------------------------
@@ -344,26 +344,33 @@ int plan_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_attention*
   const int64_t fresh = a->starts ? std::min(a->max_new, a->n_tokens) : 1;
   const int64_t rows = fresh * groups;
   p->rows = a->n_tokens * a->q_heads;
-  p->tile = rows <= 16 ? 16 : 32;
+  // Row tiles of 16, or of 32 where they would be more than half empty otherwise: 8 heads of 128 over 16 x 4096 positions with 16 rows
+  // each 35 us in tiles of 16 and 37 in tiles of 32, with 24 rows 43 and 38, with 48 71 and 50.  Lines of 256 leave the tiles of 32
+  // half the waves: with 32 rows 74 and 82 us, with 48 117 and 109.
+  p->tile = rows <= 16 || (c->vol == 256 && rows <= 32) ? 16 : 32;
   const int64_t tiles = (rows + p->tile - 1) / p->tile;
+  // A workgroup's waves share what they can of the positions: three or four row tiles go through them together (128 rows as above: 76 us,
+  // 85 wave by wave), fewer leave waves for other splits, which are joined before they are stored.
+  p->waves_rows = tiles >= 3 ? 4 : tiles == 2 ? 2 : 1;
+  p->tall = c->vol >= 64 && p->tile == 32 && p->waves_rows == 4;
+  const int waves_splits = 4 / p->waves_rows;
   int64_t length = a->max_pages * cache->page_size;
   if (a->max_length > 0) length = std::min(length, a->max_length);
   if (a->window > 0) length = std::min(length, a->window + fresh + 63);
-  // splits of the positions, where rows alone do not fill the chip
-  const int64_t alone = a->n_seqs * cache->heads * tiles;
-  int64_t splits = alone >= kComputeWaves ? 1 : (kComputeWaves + alone - 1) / alone;
-  const int waves_rows = tiles >= 4 ? 4 : tiles >= 2 ? 2 : 1;
-  splits = std::max<int64_t>(1, std::min<int64_t>({splits, kMaxSplits * (4 / waves_rows), length / 128}));
+  // Splits of the positions, where rows alone do not fill the chip: a chunk of 256 after 8192 takes 85 us with 1024 waves, 74 with 2048 and 89
+  // with 4096; the tall kernel for lines of 256 has one wave to a SIMD (32 rows after 16 x 4096: 155 us with 1024, 174 with 2048).  Down to
+  // 64 positions: one token after 8000 takes 18 us, 21 with at least 128 and 23 with 256.
+  const int64_t alone = a->n_seqs * cache->heads * tiles, busy = p->tall && c->vol == 256 ? kBusyWaves / 2 : kBusyWaves;
+  int64_t splits = std::max<int64_t>((busy + alone - 1) / alone, waves_splits);
+  splits = std::max<int64_t>(1, std::min<int64_t>({splits, kMaxSplits * waves_splits, length / 64}));
   p->chunk = ((length + splits - 1) / splits + 63) / 64 * 64;
   p->n_splits = (length + p->chunk - 1) / p->chunk;
-  p->waves_rows = p->n_splits == 1 ? 4 : waves_rows;
-  const int waves_splits = 4 / p->waves_rows;
   p->row_blocks = (tiles + p->waves_rows - 1) / p->waves_rows;
   p->split_blocks = (p->n_splits + waves_splits - 1) / waves_splits;
   p->records = p->split_blocks;
-  p->tall = c->vol >= 64 && p->tile == 32 && p->waves_rows == 4 && tiles >= 3;
-  const int wave_rows = 64 / (c->vol / 16);
-  p->finish_rows = p->records > 16 && p->rows < 4096 ? 1 : p->rows < 16384 ? wave_rows : 4 * wave_rows;
+  // Joining: few rows of many records have a workgroup each, whose threads share the records (32 rows of 131072 positions: 54 us in all, 64 with
+  // several rows to a workgroup); with 4096 rows that is the slower way (62 and 56).
+  p->finish_rows = p->records >= 8 && p->rows < 2048 ? 1 : 64 / (c->vol / 16);
   if (p->row_blocks > INT32_MAX / (a->n_seqs * cache->heads) / p->split_blocks) return PBZ_ERR_SHAPE;
   p->q_bytes = padded(uint64_t(p->rows) * 2 * c->vol);
   p->scale_bytes = padded(uint64_t(p->rows) * sizeof(float));
@@ -555,11 +562,9 @@ int pbz_cache_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_atten
   finish.wide = call.out_wide;
   finish.n_splits = int32_t(p.records);
   for_line(c->transform, c->vol, [&](auto tf, auto dim) {
-    constexpr int kTf = decltype(tf)::value, D = decltype(dim)::value, kWave = 64 / (D / 16), kBlock = 4 * kWave;
-    const auto blocks = [&](int rows) { return dim3(unsigned((p.rows + rows - 1) / rows)); };
-    if (p.finish_rows == 1) k_finish<kTf, D, 1><<<blocks(1), 256, 0, s>>>(finish);
-    else if (p.finish_rows == kWave) k_finish<kTf, D, kWave><<<blocks(kWave), 256, 0, s>>>(finish);
-    else k_finish<kTf, D, kBlock><<<blocks(kBlock), 256, 0, s>>>(finish);
+    constexpr int kTf = decltype(tf)::value, D = decltype(dim)::value, kWave = 64 / (D / 16);
+    if (p.finish_rows == 1) k_finish<kTf, D, 1><<<dim3(unsigned(p.rows)), 256, 0, s>>>(finish);
+    else k_finish<kTf, D, kWave><<<dim3(unsigned((p.rows + kWave - 1) / kWave)), 256, 0, s>>>(finish);
   });
   return hip_status(hipGetLastError());
 }
