@@ -598,3 +598,11 @@ def test_a_captured_step():
             assert torch.equal(p, r)
         n = lengths.tolist()
         check_attend(cache, q, out, None, [t[:-(-m // 16)] for t, m in zip(tables, n)], n, [1, 1])
+
+
+def test_the_example_layer():
+    """The example's layer on a compressed cache against the same one uncompressed.  Binning moves a coefficient by up to N / 254, a key or value
+    by up to sqrt(D) N / 254, which for the example's normal lines (N about 3 of a norm of sqrt(D)) is 3 sqrt(128) / 254 = 0.13 of its norm at most and
+    a third of that (uniform) on the whole: 0.05 for values and, through scores of that much, less for weights."""
+    from paper_2406_11209_amd.examples import paged_cache
+    assert paged_cache.main(tokens=300, steps=3) < 0.13
