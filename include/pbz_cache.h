@@ -67,7 +67,8 @@ int pbz_cache_copy_pages(const pbz_codec* codec, const pbz_cache* cache, int64_t
  * 0 <= j < lengths[b]; a row that sees nothing is zero, its lse -infinity.  Rows of no sequence are zero, too.
  * Query head g reads the cache's head g / (q_heads / heads).
  * What is outside its bounds is not read: table entries outside the pool hide their positions, lengths beyond the table
- * are cut to it, starts to n_tokens.  Hidden positions' contents, whatever they are, do not reach the result; a line with
+ * are cut to it, starts to n_tokens.  Hidden positions' contents, whatever they are, do not reach the result (a finite N that
+ * other rows see may choose the power of two by which weights are scaled before they are rounded, no more); a line with
  * an N that is not finite makes the rows that see it not finite.
  * Arithmetic: a query row is transformed in FP32 and held in 16-bit fixed point relative to its largest coefficient;
  * products with F are exact in integers; scores, running maxima and sums, and the output's sums are FP32; a weight

@@ -360,7 +360,9 @@ int plan_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_attention*
   // Splits of the positions, where rows alone do not fill the chip: a chunk of 256 after 8192 takes 85 us with 1024 waves, 74 with 2048 and 89
   // with 4096; the tall kernel for lines of 256 has one wave to a SIMD (32 rows after 16 x 4096: 155 us with 1024, 174 with 2048).  Down to
   // 64 positions: one token after 8000 takes 18 us, 21 with at least 128 and 23 with 256.
-  const int64_t alone = a->n_seqs * cache->heads * tiles, busy = p->tall && c->vol == 256 ? kBusyWaves / 2 : kBusyWaves;
+  // (max_new bounds the tiles of every sequence, all rows together those of all)
+  const int64_t some = std::min(a->n_seqs * tiles, (a->n_tokens * groups + p->tile - 1) / p->tile + a->n_seqs);
+  const int64_t alone = some * cache->heads, busy = p->tall && c->vol == 256 ? kBusyWaves / 2 : kBusyWaves;
   int64_t splits = std::max<int64_t>((busy + alone - 1) / alone, waves_splits);
   splits = std::max<int64_t>(1, std::min<int64_t>({splits, kMaxSplits * waves_splits, length / 64}));
   p->chunk = ((length + splits - 1) / splits + 63) / 64 * 64;
