@@ -81,12 +81,6 @@ __device__ __forceinline__ uint32_t two_values(uint32_t bytes) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-// a workgroup's place in the order of the work: neighbours in that order share keys, and go to one die
-__device__ __forceinline__ uint32_t work_index(uint32_t blocks) {
-  const uint32_t per_die = (blocks + 7) / 8;
-  return (blockIdx.x % 8) * per_die + blockIdx.x / 8;
-}
-
 // What a workgroup works on: a sequence's rows and positions, cut to what the arrays have, and a head of the cache.
 struct Part {
   int head, split, record;
@@ -97,15 +91,27 @@ struct Part {
   // (the constant address space: uniform reads through the scalar cache)
   const __attribute__((address_space(4))) int32_t* table;
 
-  __device__ __forceinline__ bool find(const AttendCall& a, int wave) {
-    const uint32_t work = work_index(a.blocks);
-    if (work >= a.blocks) return false;
-    row_block = a.row_blocks - 1 - work % a.row_blocks;      // the longest rows of a causal prompt first
-    const uint32_t split_block = work / a.row_blocks % a.split_blocks;
-    const uint32_t head_of_all = work / a.row_blocks / a.split_blocks;
-    head = int(head_of_all % uint32_t(a.cache.heads));
-    seq = head_of_all / uint32_t(a.cache.heads);
-    record = int(split_block);
+  // The workgroup's number among `units` of every head and split.  Heads in turn where there are as many as dies (every eighth workgroup is
+  // on the same one), so that the workgroups with the same keys share a die's cache and long sequences spread over the dies; with other
+  // numbers of heads, a die has a run of units of a head.
+  __device__ __forceinline__ uint32_t number(const AttendCall& a) {
+    const uint32_t heads = uint32_t(a.cache.heads), all = a.units * a.split_blocks * heads;
+    uint32_t work = blockIdx.x;
+    if (heads % 8 != 0) {
+      work = blockIdx.x % 8 * ((all + 7) / 8) + blockIdx.x / 8;
+      if (blockIdx.x / 8 >= (all + 7) / 8 || work >= all) return ~0u;
+      head = int(work / (a.units * a.split_blocks));
+      work %= a.units * a.split_blocks;
+    } else {
+      head = int(work % heads);
+      work /= heads;
+    }
+    record = int(work % a.split_blocks);
+    return work / a.split_blocks;
+  }
+  // the rest, of a sequence
+  __device__ __forceinline__ void look_at(const AttendCall& a, int64_t sequence, int wave) {
+    seq = sequence;
     split = record * (4 / a.waves_rows) + wave / a.waves_rows;
     int64_t last = seq + 1;
     first = seq;
@@ -120,7 +126,52 @@ struct Part {
     length = int(asked < 0 ? 0 : asked > a.table_tokens ? a.table_tokens : asked);
     rows = uint32_t(fresh) * uint32_t(a.groups);             // (fewer than 2^31 rows of q altogether)
     table = (const __attribute__((address_space(4))) int32_t*)(a.table + seq * a.table_stride);
+  }
+  // Units: row_blocks to every sequence.
+  __device__ __forceinline__ bool find(const AttendCall& a, int wave) {
+    const uint32_t unit = number(a);
+    if (unit == ~0u) return false;
+    row_block = unit % a.row_blocks;
+    look_at(a, unit / a.row_blocks, wave);
     return true;
+  }
+  // Units: as many to a sequence as it has runs of `block` rows, by the sums over the sequences before; 64 of them at a time.  (With as many to all
+  // as the longest has, a batch of 63 single tokens and a chunk of 512 spent most of its 690 us on workgroups with nothing to do.)
+  __device__ __forceinline__ bool find_run(const AttendCall& a, uint32_t block, int lane) {
+    uint32_t unit = number(a);
+    if (unit == ~0u) return false;
+    if (!a.starts) {
+      const uint32_t each = (uint32_t(a.groups) + block - 1) / block;
+      if (unit / each >= uint64_t(a.n_seqs)) return false;
+      row_block = each - 1 - unit % each;
+      look_at(a, unit / each, 0);
+      return true;
+    }
+    for (int64_t base = 0; base < a.n_seqs; base += 64) {
+      uint32_t runs = 0;
+      if (base + lane < a.n_seqs) {
+        int64_t from = a.starts[base + lane], to = a.starts[base + lane + 1];
+        from = from < 0 ? 0 : from;
+        to = to > a.n_tokens ? a.n_tokens : to;
+        if (to > from) runs = (uint32_t(to - from) * uint32_t(a.groups) + block - 1) / block;
+      }
+      uint32_t sum = runs;
+      for (int apart = 1; apart < 64; apart <<= 1) {
+        const uint32_t other = __shfl_up(sum, apart);
+        if (lane >= apart) sum += other;
+      }
+      const uint64_t behind = __ballot(sum > unit);
+      if (behind) {
+        const int at = __ffsll((long long)behind) - 1;
+        const uint32_t own = uint32_t(__builtin_amdgcn_readlane(int(runs), at));
+        const uint32_t before = uint32_t(__builtin_amdgcn_readlane(int(sum), at)) - own;
+        row_block = own - 1 - (unit - before);               // the longest rows of a causal prompt first
+        look_at(a, base + at, 0);
+        return true;
+      }
+      unit -= uint32_t(__builtin_amdgcn_readlane(int(sum), 63));
+    }
+    return false;
   }
 };
 
@@ -533,19 +584,17 @@ __device__ __forceinline__ void write_results(const AttendCall& a, const Part& p
   }
 }
 
-// Rows of no sequence, before the first and behind the last, are zero: the first and the last sequence's workgroups see to them.
-__device__ __forceinline__ void zero_rest(const AttendCall& a, const Part& part, int dim) {
-  if (!a.starts || part.row_block != 0 || part.record != 0) return;
+// Rows of no sequence, before the first and behind the last, are zero: a head's first workgroup sees to them.
+__device__ __forceinline__ void zero_rest(const AttendCall& a, int head, int dim) {
   for (int side = 0; side < 2; ++side) {
-    if (part.seq != (side ? a.n_seqs - 1 : 0)) continue;
     int64_t from = side ? a.starts[a.n_seqs] : 0, to = side ? a.n_tokens : a.starts[0];
     from = from < 0 ? 0 : from;
     to = to > a.n_tokens ? a.n_tokens : to;
     for (int64_t token = from; token < to; ++token)
       for (int i = threadIdx.x; i < a.groups * dim; i += 256) {
-        const int64_t head = int64_t(part.head) * a.groups + i / dim;
-        static_cast<uint16_t*>(a.out)[token * a.out_token_stride + head * a.out_head_stride + i % dim] = 0;
-        if (a.lse && i % dim == 0) a.lse[token * a.q_heads + head] = kNegInf;
+        const int64_t row_head = int64_t(head) * a.groups + i / dim;
+        static_cast<uint16_t*>(a.out)[token * a.out_token_stride + row_head * a.out_head_stride + i % dim] = 0;
+        if (a.lse && i % dim == 0) a.lse[token * a.q_heads + row_head] = kNegInf;
       }
   }
 }
@@ -778,11 +827,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, half = lane >> 5;
   Part part;
-  if (!part.find(a, 0)) return;
-  if (a.records == 1) zero_rest(a, part, D);
-  const uint32_t apart = a.row_blocks * 128;
+  if (a.records == 1 && a.starts && blockIdx.x < uint32_t(a.cache.heads)) zero_rest(a, int(blockIdx.x), D);
+  if (!part.find_run(a, 128, lane)) return;
   TallRows<D, kFine> rows;
-  for (uint32_t first = part.row_block * 128; first < part.rows; first += apart) {
+  {
+    const uint32_t first = part.row_block * 128;
     const Range all(a, part, first, part.rows - first < 128 ? part.rows - first : 128);
     const int64_t start = (all.from & ~63) + int64_t(part.split) * a.chunk;
     const int begin = start < all.to ? int(start) : all.to;
@@ -938,13 +987,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
     }
     const int at_end = this_lane();
     rows.store(a, part, own, reinterpret_cast<float*>(memory) + wave * kRoom, at_end & 31, at_end >> 5);
-    __syncthreads();
   }
 }
 
 template <int D, int kN>
 int launch(bool tall, int rows, bool fine, const AttendCall& call, hipStream_t s) {
-  const dim3 grid((call.blocks + 7) / 8 * 8), block(256);
+  const uint32_t all = call.units * call.split_blocks * uint32_t(call.cache.heads);
+  const dim3 grid((all + 7) / 8 * 8), block(256);
   if (tall) {
     if constexpr (D >= 64) {
       if (fine) k_attend_tall<D, true, kN><<<grid, block, 0, s>>>(call);

@@ -317,7 +317,7 @@ struct AttendPlan {
   int64_t rows;            // of q
   int tile;                // query rows to a wave
   int waves_rows;
-  int64_t row_blocks, split_blocks;
+  int64_t row_blocks, split_blocks, units;
   int64_t n_splits, chunk;
   int64_t records;         // splits as they are left to be joined
   int finish_rows;         // rows to a workgroup there
@@ -373,7 +373,9 @@ int plan_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_attention*
   // Joining: few rows of many records have a workgroup each, whose threads share the records (32 rows of 131072 positions: 54 us in all, 64 with
   // several rows to a workgroup); with 4096 rows that is the slower way (62 and 56).
   p->finish_rows = p->records >= 8 && p->rows < 2048 ? 1 : 64 / (c->vol / 16);
-  if (p->row_blocks > INT32_MAX / (a->n_seqs * cache->heads) / p->split_blocks) return PBZ_ERR_SHAPE;
+  // the kernel for many rows finds runs of 128 rows of every sequence; there are no more of them than
+  p->units = p->tall ? a->n_tokens * groups / 128 + a->n_seqs : a->n_seqs * p->row_blocks;
+  if (p->units > INT32_MAX / cache->heads / p->split_blocks) return PBZ_ERR_SHAPE;
   p->q_bytes = padded(uint64_t(p->rows) * 2 * c->vol);
   p->scale_bytes = padded(uint64_t(p->rows) * sizeof(float));
   p->state_bytes = p->whole() ? 0 : padded(uint64_t(p->rows) * p->records * sizeof(float2));
@@ -546,7 +548,7 @@ int pbz_cache_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_atten
   call.waves_rows = p.waves_rows;
   call.row_blocks = uint32_t(p.row_blocks);
   call.split_blocks = uint32_t(p.split_blocks);
-  call.blocks = uint32_t(p.row_blocks * p.split_blocks * a->n_seqs * cache->heads);
+  call.units = uint32_t(p.units);
   st = launch_attend(c->vol, p.tall, p.tile, a->type == PBZ_F16, call, s);
   if (st != PBZ_OK || p.whole()) return st;
 

@@ -49,7 +49,7 @@ struct AttendCall {
   int32_t n_splits;
   int32_t waves_rows;      // of a workgroup's four waves: so many take row tiles, the others splits
   uint32_t row_blocks, split_blocks;
-  uint32_t blocks;
+  uint32_t units;          // workgroups of a head and a split
 };
 
 // tall: the kernel for many rows; rows: query rows to a wave, 16 or 32; a translation unit per D
