@@ -221,6 +221,57 @@ struct Keys {
   }
 };
 
+// The lane, of which the compiler must not know that it is the same every time: what is derived from it before and after the pass over the
+// positions would otherwise be kept in registers during it, where there are none to spare.
+__device__ __forceinline__ int this_lane() {
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+
+// Results of 16 rows, first ..: a wave's coefficients, from LDS, transformed back and written.
+template <int D>
+constexpr int kResultPitch = D + 4;
+template <int D>
+__device__ __forceinline__ void write_results(const AttendCall& a, const Part& part, uint32_t first, const float* staged) {
+  constexpr int L = D / 16, kLines = 64 / L < 16 ? 64 / L : 16;
+  const int lane = this_lane(), in_line = lane % L;
+  const uint32_t groups = uint32_t(a.groups);
+#pragma unroll 1
+  for (int base = 0; base < 16 && first + base < part.rows; base += kLines) {
+    const int line = base + lane / L < 16 ? base + lane / L : 15;
+    float v[16];
+    if (a.transform == PBZ_TRANSFORM_HAAR) {
+#pragma unroll
+      for (int k = 0; k < 16; ++k) v[k] = staged[line * kResultPitch<D> + line::coefficient<kTfHaar, L>(in_line, k)];
+      line::inverse<kTfHaar, float, L>(v, lane);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 16; ++k) v[k] = staged[line * kResultPitch<D> + line::coefficient<kTfDct, L>(in_line, k)];
+      line::inverse<kTfDct, float, L>(v, lane);
+    }
+    const uint32_t row = first + line, token = row / groups;
+    if (row < part.rows && base + lane / L < 16)
+      store_run(static_cast<uint16_t*>(a.out) + (part.first + token) * a.out_token_stride +
+                    (int64_t(part.head) * groups + (row - token * groups)) * a.out_head_stride + in_line * 16, a.type, a.out_wide != 0, v);
+  }
+}
+
+// Rows of no sequence, before the first and behind the last, are zero: a head's first workgroup sees to them.
+__device__ __forceinline__ void zero_rest(const AttendCall& a, int head, int dim) {
+  for (int side = 0; side < 2; ++side) {
+    int64_t from = side ? a.starts[a.n_seqs] : 0, to = side ? a.n_tokens : a.starts[0];
+    from = from < 0 ? 0 : from;
+    to = to > a.n_tokens ? a.n_tokens : to;
+    for (int64_t token = from; token < to; ++token)
+      for (int i = threadIdx.x; i < a.groups * dim; i += 256) {
+        const int64_t row_head = int64_t(head) * a.groups + i / dim;
+        static_cast<uint16_t*>(a.out)[token * a.out_token_stride + row_head * a.out_head_stride + i % dim] = 0;
+        if (a.lse && i % dim == 0) a.lse[token * a.q_heads + row_head] = kNegInf;
+      }
+  }
+}
+
 // A wave's 16 R rows of one head: what it keeps of them while positions go by, 32 to a step.
 template <int D, int R, bool kFine, int kN>
 struct Rows {
@@ -425,16 +476,30 @@ struct Rows {
     }
   }
 
-  // a lane has coefficients (4 quarter + i) DT + t of its rows
-  __device__ __forceinline__ void store(const AttendCall& a, int record, int quarter) {
+  // a lane has coefficients (4 quarter + i) DT + t of its rows: a record, or where there are no splits the result, by way of the wave's
+  // room in LDS
+  __device__ __forceinline__ void store(const AttendCall& a, const Part& part, uint32_t first_row, float* staged, int c, int quarter) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float l = total[r];
       l += __shfl_xor(l, 16);
       l += __shfl_xor(l, 32);
-      if (place[r] < 0) continue;
       if (l != l) top[r] = 0.f;            // a row that sees a NaN is one, also where it sees nothing else
-      const int64_t to = int64_t(record) * a.n_tokens * a.q_heads + place[r];
+      if (a.records == 1) {
+        if (a.lse && quarter == 0 && place[r] >= 0) a.lse[place[r]] = (top[r] + __builtin_amdgcn_logf(l)) * 0.693147180559945309f;
+        const float by = top[r] == kNegInf ? 0.f : 1.f / l;
+        float* to = staged + c * kResultPitch<D> + quarter * 4 * DT;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int t = 0; t < DT; ++t) to[i * DT + t] = sum[r][t][i] * by;
+        wave_lds_sync();
+        write_results<D>(a, part, first_row + r * 16, staged);
+        wave_lds_sync();
+        continue;
+      }
+      if (place[r] < 0) continue;
+      const int64_t to = int64_t(part.record) * a.n_tokens * a.q_heads + place[r];
       if (quarter == 0) a.space.state[to] = make_float2(top[r], l);
       if (top[r] == kNegInf) continue;
       float* out = a.space.sums + to * D + quarter * 4 * DT;
@@ -478,7 +543,8 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
   if (!part.find(a, wave)) return;
   const int sharing = 4 / a.waves_rows;          // waves with the same rows, whose splits become one record
   Rows<D, R, kFine, kN> rows;
-  __shared__ float left[3][Rows<D, R, kFine, kN>::kLeft * 64];
+  __shared__ float left[D == 32 ? 4 : 3][Rows<D, R, kFine, kN>::kLeft * 64];      // (with more columns, at most two waves have rows)
+  if (a.records == 1 && a.starts && part.seq == 0 && part.row_block == 0) zero_rest(a, part.head, D);
   const uint32_t together = uint32_t(a.waves_rows) * (16 * R);
   for (uint32_t base = part.row_block * together; base < part.rows; base += a.row_blocks * together) {
     const uint32_t first = base + uint32_t(wave % a.waves_rows) * (16 * R);
@@ -542,60 +608,11 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
     if (turn == 0) {
       rows.into_unit();
       for (int w = 1; w < sharing; ++w) rows.take(left[wave + (w - 1) * a.waves_rows], lane);
-      rows.store(a, part.record, quarter);
+      wave_lds_sync();
+      const int at_end = this_lane();
+      rows.store(a, part, first, left[wave], at_end & 15, at_end >> 4);
     }
     if (sharing > 1) __syncthreads();
-  }
-}
-
-// The lane, of which the compiler must not know that it is the same every time: what is derived from it before and after the pass over the
-// positions would otherwise be kept in registers during it, where there are none to spare.
-__device__ __forceinline__ int this_lane() {
-  int lane = threadIdx.x & 63;
-  asm volatile("" : "+v"(lane));
-  return lane;
-}
-
-// Results of 16 rows, first ..: a wave's coefficients, from LDS, transformed back and written.
-template <int D>
-constexpr int kResultPitch = D + 4;
-template <int D>
-__device__ __forceinline__ void write_results(const AttendCall& a, const Part& part, uint32_t first, const float* staged) {
-  constexpr int L = D / 16, kLines = 64 / L < 16 ? 64 / L : 16;
-  const int lane = this_lane(), in_line = lane % L;
-  const uint32_t groups = uint32_t(a.groups);
-#pragma unroll 1
-  for (int base = 0; base < 16 && first + base < part.rows; base += kLines) {
-    const int line = base + lane / L < 16 ? base + lane / L : 15;
-    float v[16];
-    if (a.transform == PBZ_TRANSFORM_HAAR) {
-#pragma unroll
-      for (int k = 0; k < 16; ++k) v[k] = staged[line * kResultPitch<D> + line::coefficient<kTfHaar, L>(in_line, k)];
-      line::inverse<kTfHaar, float, L>(v, lane);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 16; ++k) v[k] = staged[line * kResultPitch<D> + line::coefficient<kTfDct, L>(in_line, k)];
-      line::inverse<kTfDct, float, L>(v, lane);
-    }
-    const uint32_t row = first + line, token = row / groups;
-    if (row < part.rows && base + lane / L < 16)
-      store_run(static_cast<uint16_t*>(a.out) + (part.first + token) * a.out_token_stride +
-                    (int64_t(part.head) * groups + (row - token * groups)) * a.out_head_stride + in_line * 16, a.type, a.out_wide != 0, v);
-  }
-}
-
-// Rows of no sequence, before the first and behind the last, are zero: a head's first workgroup sees to them.
-__device__ __forceinline__ void zero_rest(const AttendCall& a, int head, int dim) {
-  for (int side = 0; side < 2; ++side) {
-    int64_t from = side ? a.starts[a.n_seqs] : 0, to = side ? a.n_tokens : a.starts[0];
-    from = from < 0 ? 0 : from;
-    to = to > a.n_tokens ? a.n_tokens : to;
-    for (int64_t token = from; token < to; ++token)
-      for (int i = threadIdx.x; i < a.groups * dim; i += 256) {
-        const int64_t row_head = int64_t(head) * a.groups + i / dim;
-        static_cast<uint16_t*>(a.out)[token * a.out_token_stride + row_head * a.out_head_stride + i % dim] = 0;
-        if (a.lse && i % dim == 0) a.lse[token * a.q_heads + row_head] = kNegInf;
-      }
   }
 }
 

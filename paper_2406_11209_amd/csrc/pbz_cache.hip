@@ -321,8 +321,8 @@ struct AttendPlan {
   int64_t n_splits, chunk;
   int64_t records;         // splits as they are left to be joined
   int finish_rows;         // rows to a workgroup there
-  bool tall;               // the kernel for many rows, which finishes what is not split by itself
-  bool whole() const { return tall && records == 1; }
+  bool tall;               // the kernel for many rows
+  bool whole() const { return records == 1; }       // the pass over the positions writes the results itself
   size_t q_bytes, scale_bytes, state_bytes, sum_bytes;
   size_t total() const { return q_bytes + scale_bytes + state_bytes + sum_bytes; }
 };
