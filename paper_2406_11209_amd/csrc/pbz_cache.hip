@@ -42,26 +42,28 @@ __global__ __launch_bounds__(256) void k_append(const AppendCall a) {
   double v[16];
   load_run(x.data, a.type, token * x.token_stride + head * x.head_stride + part * 16, a.wide != 0, v);
   const int64_t slot = a.slots[token];
-  const bool finite = line_finite<double, L>(v);
   line::forward<kTf, double, L>(v, lane);
   const double N = line_max<double, L>(v);
-  // Quotients as products with a reciprocal, off by some 2^-45 at most; next to a border between two indices the quotient itself decides.
+  const bool finite = N < __builtin_huge_val();
+  // Quotients as products with a reciprocal, off by some 2^-45 at most; next to a border between two indices the quotient itself decides.  Adding
+  // 1.5 * 2^52 leaves the nearest integer in the sum's lowest bits.
   const double reciprocal = N > 0.0 && finite ? 127.0 / N : 0.0;
-  double r[16];
+  int r[16];
   bool close = false;
 #pragma unroll
   for (int k = 0; k < 16; ++k) {
-    const double q = v[k] * reciprocal;
-    r[k] = rint(q);
-    close = close || fabs(q - r[k]) > 0.5 - 0x1p-30;
+    v[k] = finite ? v[k] : 0.0;
+    const double sum = fma(v[k], reciprocal, 0x1.8p52);
+    r[k] = int(uint32_t(__builtin_bit_cast(uint64_t, sum)));
+    close = close || fabs(fma(v[k], reciprocal, 0x1.8p52 - sum)) > 0.5 - 0x1p-30;
   }
   if (close) {
-#pragma unroll
-    for (int k = 0; k < 16; ++k) r[k] = reciprocal > 0.0 ? rint(127.0 * v[k] / N) : 0.0;
+#pragma unroll 1
+    for (int k = 0; k < 16; ++k) r[k] = reciprocal > 0.0 ? int(rint(127.0 * v[k] / N)) : 0;
   }
   uint8_t* bytes = reinterpret_cast<uint8_t*>(staged[wave]) + in_wave * kPitch;
 #pragma unroll
-  for (int k = 0; k < 16; ++k) bytes[line::coefficient<kTf, L>(part, k)] = uint8_t(int(r[k]));
+  for (int k = 0; k < 16; ++k) bytes[line::coefficient<kTf, L>(part, k)] = uint8_t(r[k]);
   wave_lds_sync();
   const int64_t page = slot >> a.cache.page_shift;
   if (!there || slot < 0 || page >= a.cache.n_pages) return;
@@ -123,35 +125,38 @@ struct QueryCall {
 // Transformed, and held relative to the row's largest coefficient in 16 bits, +-32639 = 127 * 256 + 127, high and low byte signed.
 template <int kTf, int D>
 __global__ __launch_bounds__(256) void k_queries(const QueryCall a) {
-  constexpr int L = D / 16, kLines = 64 / L, kPitch = 2 * D + 4;
-  __shared__ uint32_t staged[4][kLines * kPitch / 4];
+  constexpr int L = D / 16, kLines = 64 / L, kPitch = D + 2;      // in coefficients of 16 bits
+  __shared__ uint32_t staged[4][kLines * kPitch / 2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane % L, in_wave = lane / L;
   const int64_t asked = (int64_t(blockIdx.x) * 4 + wave) * kLines + in_wave;
   const bool there = asked < a.rows;
   const int64_t row = there ? asked : a.rows - 1;
   const int64_t token = row / a.q_heads;
   float v[16];
-  load_run(a.q, a.type, token * a.token_stride + (row - token * a.q_heads) * a.head_stride + part * 16, a.wide != 0, v);
-  const bool finite = line_finite<float, L>(v);
+  load_run_16(a.q, a.type, token * a.token_stride + (row - token * a.q_heads) * a.head_stride + part * 16, a.wide != 0, v);
   line::forward<kTf, float, L>(v, lane);
   const float most = line_max<float, L>(v);
-  const float up = finite && most > 0.f ? 32639.f / most : 0.f;
-  const float sign = a.scale < 0.f ? -1.f : 1.f;
-  uint8_t* bytes = reinterpret_cast<uint8_t*>(staged[wave]) + in_wave * kPitch;
+  const bool finite = most < __builtin_huge_valf();
+  float up = finite && most > 0.f ? 32639.f / most : 0.f;
+  up = up < __builtin_huge_valf() ? a.scale < 0.f ? -up : up : 0.f;
+  // Adding 1.5 * 2^23 leaves the nearest integer in the sum's lowest bits; and 128, for the high byte to be signed's and the low one's bit 7 the
+  // other way round.
+  uint16_t* both = reinterpret_cast<uint16_t*>(staged[wave]) + in_wave * kPitch;
 #pragma unroll
-  for (int k = 0; k < 16; ++k) {
-    const int index = up < __builtin_huge_valf() ? int(rintf(fminf(fmaxf(v[k] * up, -32639.f), 32639.f) * sign)) : 0;
-    const int high = (index + 128) >> 8;
-    const int at = line::coefficient<kTf, L>(part, k);
-    bytes[at] = uint8_t(high);
-    bytes[D + at] = uint8_t(index - 256 * high);
-  }
+  for (int k = 0; k < 16; ++k) both[line::coefficient<kTf, L>(part, k)] = uint16_t(__float_as_uint(fmaf(v[k], up, 0x1.8p23f + 128.f)));
   wave_lds_sync();
   if (!there) return;
-  const uint32_t* from = staged[wave] + (in_wave * kPitch + part * 32) / 4;
-  uint4* q = reinterpret_cast<uint4*>(a.space.q + row * (2 * D) + part * 32);
+  const uint32_t* from = staged[wave] + (in_wave * kPitch + part * 16) / 2;
+  uint32_t high[4], low[4];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) q[i] = make_uint4(from[4 * i], from[4 * i + 1], from[4 * i + 2], from[4 * i + 3]);
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w0 = from[2 * i], w1 = from[2 * i + 1];
+    high[i] = __builtin_amdgcn_perm(w1, w0, 0x07050301u);
+    low[i] = __builtin_amdgcn_perm(w1, w0, 0x06040200u) ^ 0x80808080u;
+  }
+  int8_t* const q = a.space.q + row * (2 * D) + part * 16;
+  *reinterpret_cast<uint4*>(q) = make_uint4(high[0], high[1], high[2], high[3]);
+  *reinterpret_cast<uint4*>(q + D) = make_uint4(low[0], low[1], low[2], low[3]);
   if (part == 0) a.space.q_scale[row] = finite ? most * (1.f / 32639.f) * fabsf(a.scale) : __builtin_nanf("");
 }
 

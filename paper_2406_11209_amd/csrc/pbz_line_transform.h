@@ -4,11 +4,16 @@
 //   s[m] = x[m] + x[n-1-m]:                          c_n[2k]   = c_{n/2}(s)[k]
 //   d[m] = (x[m] - x[n-1-m]) / (2 cos(pi (2m+1) / (2n))):  c_n[2k+1] = c_{n/2}(d)[k] + c_{n/2}(d)[k+1]
 // the latter because 2 cos(t) cos((2k+1) t) = cos(2k t) + cos(2(k+1) t).  With lane l holding x[16 l ..], x[n-1-m] is in the
-// mirrored lane, so a split is one exchange with it, after which the lower half of the lanes has s and the upper half, in mirrored
-// order, has d; log2(L) splits leave every lane a line of 16, which the in-register transform of pbz_dct.h takes.  The sums over
-// k and k + 1 are again with one neighbour each.  Exchanges among up to eight lanes are register moves (the neighbours' sums of 16 lanes
+// mirrored lane, so a split is one exchange with it, after which the lower half of the lanes has s and the upper half d: a value, plus or minus
+// the mirrored lane's, times a lane's factor.  Then the upper half's lanes are in mirrored order, and so are the values within each.  log2(L)
+// splits leave every lane a line of 16, which the in-register transform of pbz_dct.h takes; where the 16 are in mirrored order, the
+// coefficients of odd index change their sign.  The sums over k and k + 1 are again with one neighbour each.  All of that is without the
+// orthonormal transform's factors: sqrt(1/2) for every split is in the lanes' factors, and the first coefficient's is set right before and after
+// the sums.  Exchanges among up to eight lanes are register moves (the neighbours' sums of 16 lanes
 // go through LDS).  The inverse is the transpose, step by step in reverse.  The factors reach n / pi, which costs that many
 // roundings' accuracy at worst: nothing in FP64, and in FP32 for n = 256 still 2^-17 of the line's norm.
+// (With selects between sums and differences, and the orthonormal factors at every step: FP64 as 9 instructions a value and split and 9 a value
+// and sum, 4 and 4 now.)
 // 16 values to a lane: with 32, one split less, but an in-register transform of 341 multiply-adds instead of 85 and twice the code, which a
 // launch over few lines fetches for nearly as long as it computes (128 keys and values of 64 tokens: 9.2 us, 6.7 with 16; over many lines the two
 // are the same).
@@ -39,18 +44,17 @@ __device__ __forceinline__ double moved(double v) {
 // DPP control of the mirrored lane among n lanes
 template <int n> struct Mirror { static constexpr int control = n == 2 ? 0xB1 : n == 4 ? 0x1B : n == 8 ? 0x141 : 0x140; };
 
-// A lane's part in the splits.  Split i is of L >> i lanes: which half of them the lane is in, its place among that half, and the index
+// A lane's part in the splits.  Split i is of L >> i lanes: which half of them the lane is in, and the index
 // that its results have among the half's, modulo the half's lanes.
 template <int L>
 struct Path {
-  int half[4] = {0, 0, 0, 0}, place[4] = {0, 0, 0, 0}, index[5] = {0, 0, 0, 0, 0};
+  int half[4] = {0, 0, 0, 0}, index[5] = {0, 0, 0, 0, 0};
   __device__ __forceinline__ explicit Path(int lane) {
     int p = lane;
 #pragma unroll
     for (int n = L, i = 0; n > 1; n >>= 1, ++i) {
       half[i] = p >= n / 2;
       p = half[i] ? n - 1 - p : p;
-      place[i] = p;
     }
 #pragma unroll
     for (int i = 3; i >= 0; --i) index[i] = i + 1 < 4 ? half[i + 1] + 2 * index[i + 1] : 0;
@@ -74,100 +78,118 @@ __device__ __forceinline__ int lane_of_index(int lane, int index) {
   return (lane & ~15) + 15 - int((0x52614370u >> (4 * (index & 7))) & 7);
 }
 
-// 1 / (2 cos(pi (2m+1) / (2n))) for m < n / 2, n = 32, 64, 128, 256 one after the other
-template <typename T>
-struct alignas(32) Secants {
-  T v[16 + 32 + 64 + 128];
-  constexpr Secants() : v() {
-    int at = 0;
-    for (int n = 32; n <= 256; n *= 2)
-      for (int m = 0; m < n / 2; ++m) v[at++] = T(0.5 / dct::cos_frac(2 * m + 1, n));
+// What the lanes' values are multiplied by at each split: sqrt(1/2), in the upper half over 2 cos(pi (2m+1) / (2n)), and negative, since it is the
+// mirrored lane's value minus its own that is wanted.
+template <typename T, int L>
+struct alignas(32) Factors {
+  static constexpr int kSplits = L == 16 ? 4 : L == 8 ? 3 : L == 4 ? 2 : 1;
+  static constexpr int kWide = 16 / sizeof(T);      // to a load; the lanes' side by side
+  T v[kSplits * L * kRun];
+  constexpr Factors() : v() {
+    for (int lane = 0; lane < L; ++lane) {
+      int place = lane;
+      bool mirrored = false;
+      for (int split = 0, n = L; split < kSplits; ++split, n /= 2) {
+        const bool upper = place >= n / 2;
+        if (upper) {
+          place = n - 1 - place;
+          mirrored = !mirrored;
+        }
+        for (int i = 0; i < kRun; ++i) {
+          const int m = place * kRun + (mirrored ? kRun - 1 - i : i);
+          v[((split * (kRun / kWide) + i / kWide) * L + lane) * kWide + i % kWide] = T(upper ? -dct::kInvSqrt2 * 0.5 / dct::cos_frac(2 * m + 1, n * kRun) : dct::kInvSqrt2);
+        }
+      }
+    }
   }
 };
-static __device__ const Secants<float> kSecantsF32 = Secants<float>();
-static __device__ const Secants<double> kSecantsF64 = Secants<double>();
-__device__ __forceinline__ const float* secants(float) { return kSecantsF32.v; }
-__device__ __forceinline__ const double* secants(double) { return kSecantsF64.v; }
+template <typename T, int L>
+static __device__ const Factors<T, L> kFactors = Factors<T, L>();
 
-// the factors of a lane at the split of n lanes (1 where it has the sums), read all at once
-template <typename T, int n>
-__device__ __forceinline__ void factors(T (&f)[kRun], int half, int place) {
-  typedef T Four __attribute__((ext_vector_type(4)));
-  const Four* table = reinterpret_cast<const Four*>(secants(T()) + (n / 2 - 1) * kRun + kRun * place);
+// a lane's factors at a split, read all at once
+template <typename T, int L>
+__device__ __forceinline__ void factors(T (&f)[kRun], int split, int lane) {
+  constexpr int kWide = Factors<T, L>::kWide;
+  typedef T Wide __attribute__((ext_vector_type(kWide)));
+  const Wide* table = reinterpret_cast<const Wide*>(kFactors<T, L>.v) + split * (kRun / kWide) * L + lane;
 #pragma unroll
-  for (int i = 0; i < kRun / 4; ++i) {
-    const Four u = table[i];
+  for (int i = 0; i < kRun / kWide; ++i) {
+    const Wide u = table[i * L];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) f[4 * i + j] = half ? u[j] : T(1);
+    for (int j = 0; j < kWide; ++j) f[kWide * i + j] = u[j];
   }
 }
 
-template <typename T, int n>       // n lanes
-__device__ __forceinline__ void split(T (&v)[kRun], int half, int place) {
+template <typename T, int n, int L>       // n lanes of L
+__device__ __forceinline__ void split(T (&v)[kRun], int which, int half, int lane) {
   T f[kRun];
-  factors<T, n>(f, half, place);
+  factors<T, L>(f, which, lane);
+  const T side = half ? T(-1) : T(1);
 #pragma unroll
   for (int i = 0; i < kRun / 2; ++i) {
     const int j = kRun - 1 - i;
     const T ti = moved<Mirror<n>::control>(v[i]), tj = moved<Mirror<n>::control>(v[j]);
-    const T si = v[i] + tj, sj = v[j] + ti, di = ti - v[j], dj = tj - v[i];
-    v[i] = (half ? di : si) * f[i];
-    v[j] = (half ? dj : sj) * f[j];
+    v[i] = (v[i] + tj * side) * f[i];
+    v[j] = (v[j] + ti * side) * f[j];
   }
 }
-template <typename T, int n>
-__device__ __forceinline__ void unsplit(T (&v)[kRun], int half, int place) {
+template <typename T, int n, int L>
+__device__ __forceinline__ void unsplit(T (&v)[kRun], int which, int half, int lane) {
   T f[kRun];
-  factors<T, n>(f, half, place);
+  factors<T, L>(f, which, lane);
+  const T side = half ? T(1) : T(-1);                     // the mirrored lane's
 #pragma unroll
   for (int i = 0; i < kRun; ++i) v[i] *= f[i];
 #pragma unroll
   for (int i = 0; i < kRun / 2; ++i) {
     const int j = kRun - 1 - i;
     const T ti = moved<Mirror<n>::control>(v[i]), tj = moved<Mirror<n>::control>(v[j]);
-    const T si = v[i] + ti, sj = v[j] + tj, di = tj - v[j], dj = ti - v[i];
-    v[i] = half ? di : si;
-    v[j] = half ? dj : sj;
+    v[i] = v[i] + tj * side;
+    v[j] = v[j] + ti * side;
   }
 }
 
-// index among the coefficients of the half: k (n / 2) + t
+// Coefficients from those of the halves: the upper half's are sums with the next one's, index k (n / 2) + t of the half's, which the lane with
+// t + 1 has, and for the last t the one with t = 0 under k + 1.
 template <typename T, int n, int L>
 __device__ __forceinline__ void join(T (&v)[kRun], int half, int t, int lane) {
-  const T r = T(dct::kInvSqrt2), first = t == 0 ? T(1) : r;      // sqrt(2) times r at index 0
-  const int source = n == 16 ? lane_of_index(lane, t + 1) : 0;
-  T next = T(0);
-  if constexpr (n > 2) next = neighbour<n, L, 1>(v[0], source, lane);
+  if constexpr (n == 2) {
+    const T with = half ? T(1) : T(0);
 #pragma unroll
-  for (int k = 0; k < kRun; ++k) {
-    T after = T(0);
-    if (k < kRun - 1) {
-      if constexpr (n > 2) after = neighbour<n, L, 1>(v[k + 1], source, lane);
-      else after = v[k + 1];
+    for (int k = 0; k < kRun - 1; ++k) v[k] = v[k] + v[k + 1] * with;
+  } else {
+    const int source = n == 16 ? lane_of_index(lane, t + 1) : 0;
+    const bool last = t == n / 2 - 1;
+    const T same = half && !last ? T(1) : T(0), above = half && last ? T(1) : T(0);
+    T next = neighbour<n, L, 1>(v[0], source, lane);
+#pragma unroll
+    for (int k = 0; k < kRun; ++k) {
+      v[k] = v[k] + next * same;
+      if (k < kRun - 1) {
+        next = neighbour<n, L, 1>(v[k + 1], source, lane);
+        v[k] = v[k] + next * above;
+      }
     }
-    const T other = n > 2 && t != n / 2 - 1 ? next : after;
-    const T own = k == 0 ? v[k] * first : v[k] * r;
-    v[k] = half ? own + other * r : v[k] * r;
-    next = after;
   }
 }
 template <typename T, int n, int L>
 __device__ __forceinline__ void unjoin(T (&v)[kRun], int half, int t, int lane) {
-  const T r = T(dct::kInvSqrt2), first = t == 0 ? T(1) : r;
-  const int source = n == 16 ? lane_of_index(lane, t - 1) : 0;
-  T previous = T(0);
-  if constexpr (n > 2) previous = neighbour<n, L, -1>(v[kRun - 1], source, lane);
+  if constexpr (n == 2) {
+    const T with = half ? T(1) : T(0);
 #pragma unroll
-  for (int k = kRun - 1; k >= 0; --k) {
-    T before = T(0);
-    if (k > 0) {
-      if constexpr (n > 2) before = neighbour<n, L, -1>(v[k - 1], source, lane);
-      else before = v[k - 1];
+    for (int k = kRun - 1; k > 0; --k) v[k] = v[k] + v[k - 1] * with;
+  } else {
+    const int source = n == 16 ? lane_of_index(lane, t - 1) : 0;
+    const T same = half && t != 0 ? T(1) : T(0), below = half && t == 0 ? T(1) : T(0);
+    T previous = neighbour<n, L, -1>(v[kRun - 1], source, lane);
+#pragma unroll
+    for (int k = kRun - 1; k >= 0; --k) {
+      v[k] = v[k] + previous * same;
+      if (k > 0) {
+        previous = neighbour<n, L, -1>(v[k - 1], source, lane);
+        v[k] = v[k] + previous * below;
+      }
     }
-    const T other = n > 2 && t != 0 ? previous : before;
-    const T own = k == 0 ? v[k] * first : v[k] * r;
-    v[k] = half ? own + other * r : v[k] * r;
-    previous = before;
   }
 }
 
@@ -189,21 +211,32 @@ __device__ __forceinline__ int coefficient(int lane, int k) {     // which one v
 template <int n, int L>
 constexpr int kLevel = L / n >= 8 ? 3 : L / n >= 4 ? 2 : L / n >= 2 ? 1 : 0;      // which split the one of n lanes is
 
+// of values in mirrored order
+template <typename T, int L>
+__device__ __forceinline__ void odd_signs(T (&v)[kRun], const Path<L>& path) {
+  const T sign = (path.half[0] + path.half[1] + path.half[2] + path.half[3]) & 1 ? T(-1) : T(1);
+#pragma unroll
+  for (int k = 1; k < kRun; k += 2) v[k] *= sign;
+}
+
 // lane: of the wave; a line's lanes start at a multiple of L
 template <int kTf, typename T, int L>
 __device__ __forceinline__ void forward(T (&v)[kRun], int lane) {
   const int part = lane % L;
   if constexpr (kTf == kTfDct) {
     const Path<L> path(part);
-    if constexpr (L >= 16) split<T, 16>(v, path.half[0], path.place[0]);
-    if constexpr (L >= 8) split<T, 8>(v, path.half[kLevel<8, L>], path.place[kLevel<8, L>]);
-    if constexpr (L >= 4) split<T, 4>(v, path.half[kLevel<4, L>], path.place[kLevel<4, L>]);
-    split<T, 2>(v, path.half[kLevel<2, L>], path.place[kLevel<2, L>]);
+    if constexpr (L >= 16) split<T, 16, L>(v, 0, path.half[0], part);
+    if constexpr (L >= 8) split<T, 8, L>(v, kLevel<8, L>, path.half[kLevel<8, L>], part);
+    if constexpr (L >= 4) split<T, 4, L>(v, kLevel<4, L>, path.half[kLevel<4, L>], part);
+    split<T, 2, L>(v, kLevel<2, L>, path.half[kLevel<2, L>], part);
     dct::forward<T, kRun, 1>(v);
+    odd_signs<T, L>(v, path);
+    v[0] *= T(2.0 * dct::kInvSqrt2);
     join<T, 2, L>(v, path.half[kLevel<2, L>], path.index[kLevel<2, L>], lane);
     if constexpr (L >= 4) join<T, 4, L>(v, path.half[kLevel<4, L>], path.index[kLevel<4, L>], lane);
     if constexpr (L >= 8) join<T, 8, L>(v, path.half[kLevel<8, L>], path.index[kLevel<8, L>], lane);
     if constexpr (L >= 16) join<T, 16, L>(v, path.half[0], path.index[0], lane);
+    v[0] *= part == 0 ? T(dct::kInvSqrt2) : T(1);
   } else {
     haar::forward<T, kRun, 1>(v);
     T sum = v[0];
@@ -222,15 +255,18 @@ __device__ __forceinline__ void inverse(T (&v)[kRun], int lane) {
   const int part = lane % L;
   if constexpr (kTf == kTfDct) {
     const Path<L> path(part);
+    v[0] *= part == 0 ? T(dct::kInvSqrt2) : T(1);
     if constexpr (L >= 16) unjoin<T, 16, L>(v, path.half[0], path.index[0], lane);
     if constexpr (L >= 8) unjoin<T, 8, L>(v, path.half[kLevel<8, L>], path.index[kLevel<8, L>], lane);
     if constexpr (L >= 4) unjoin<T, 4, L>(v, path.half[kLevel<4, L>], path.index[kLevel<4, L>], lane);
     unjoin<T, 2, L>(v, path.half[kLevel<2, L>], path.index[kLevel<2, L>], lane);
+    odd_signs<T, L>(v, path);
+    v[0] *= T(2.0 * dct::kInvSqrt2);
     dct::inverse<T, kRun, 1, kRun>(v);
-    unsplit<T, 2>(v, path.half[kLevel<2, L>], path.place[kLevel<2, L>]);
-    if constexpr (L >= 4) unsplit<T, 4>(v, path.half[kLevel<4, L>], path.place[kLevel<4, L>]);
-    if constexpr (L >= 8) unsplit<T, 8>(v, path.half[kLevel<8, L>], path.place[kLevel<8, L>]);
-    if constexpr (L >= 16) unsplit<T, 16>(v, path.half[0], path.place[0]);
+    unsplit<T, 2, L>(v, kLevel<2, L>, path.half[kLevel<2, L>], part);
+    if constexpr (L >= 4) unsplit<T, 4, L>(v, kLevel<4, L>, path.half[kLevel<4, L>], part);
+    if constexpr (L >= 8) unsplit<T, 8, L>(v, kLevel<8, L>, path.half[kLevel<8, L>], part);
+    if constexpr (L >= 16) unsplit<T, 16, L>(v, 0, path.half[0], part);
   } else {
     T value = v[0];
 #pragma unroll
