@@ -66,8 +66,8 @@ def build(verbose: bool = False) -> str:
     headers = sysconfig.get_paths()["include"]
     if os.path.exists(os.path.join(headers, "Python.h")):
         host_cc = [shutil.which("gcc") or shutil.which("cc") or cc, "-x", "c"]
-        _run(host_cc + ["-O2", "-std=c11", "-Wall", "-Werror", "-shared", "-fPIC", "-I" + headers, os.path.join(CSRC, "pbz_binding.c"),
-                        "-o", BINDING + ".tmp"])
+        _run(host_cc + ["-O2", "-std=c11", "-Wall", "-Werror", "-shared", "-fPIC", "-I" + headers, "-I" + os.path.join(ROOT, "include"),
+                        os.path.join(CSRC, "pbz_binding.c"), "-o", BINDING + ".tmp"])
         os.replace(BINDING + ".tmp", BINDING)
     else:
         if os.path.exists(BINDING):

@@ -74,6 +74,7 @@ def _library():
             fn = getattr(lib, name)
             fn.restype = res
             fn.argtypes = args
+            lib.addresses[name] = _c.cast(fn, _p).value
         _declared = lib
     return lib
 
@@ -171,7 +172,11 @@ class PagedCache:
         for name, pool in zip(("k_N", "k_F", "v_N", "v_F"), self.pools):
             setattr(self._struct, name, api._ptr(pool))
         self.device = self.k_N.device
-        self._spaces = {}            # stream -> workspace
+        self._spaces = {}            # stream -> workspace, its bytes
+        # for the native side of the calls: entry points, codec and pools, and what tensors are held against
+        self._append, self._copy, self._attend = (self._lib.addresses["pbz_cache_" + name] for name in ("append", "copy_pages", "attend"))
+        self._handle, self._at = self._h.value, _c.addressof(self._struct)
+        self._held = (self.device, torch.int32, torch.int64, torch.float32, self.heads, self.head_dim)
         self._need = {}              # sizes of an attention call -> bytes of its workspace
 
     @property
@@ -181,41 +186,20 @@ class PagedCache:
         n_type = api._torch_ftype(self.codec.work_type)
         return [(lines, n_type), (lines + (self.head_dim,), torch.int8)] * 2
 
-    # ---- calls on tensors ------------------------------------------------------------------
-    def _lines(self, x, tokens: Optional[int], heads: int, name: str):
-        if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != self.head_dim or (tokens is not None and x.shape[0] != tokens):
-            raise ValueError(f"{name} has to be [tokens, {heads}, {self.head_dim}], not {tuple(x.shape)}")
-        if x.device != self.device:
-            raise ValueError(f"{name} is not on the cache's device")
-        token, head, element = x.stride()
-        if element != 1:
-            raise ValueError(f"{name}'s last dimension has to be contiguous")
-        return token, head
-
-    def _indices(self, t, dtype, shape, name: str) -> int:
-        if t.dtype != dtype or tuple(t.shape) != shape or t.device != self.device or not t.is_contiguous():
-            raise ValueError(f"{name} has to be a contiguous {dtype} tensor of shape {shape} on the cache's device")
-        return t.data_ptr()
-
+    # ---- calls on tensors (checked and handed over by csrc/pbz_binding.c) --------------------
     def append(self, k, v, slots) -> None:
         """pbz_cache_append: compress keys and values [tokens, heads, head_dim] into their slots (int64, device;
         page * page_size + place, -1 leaves a token out)."""
-        torch = api._torch()
-        tokens = k.shape[0]
-        if k.dtype != v.dtype or k.dtype not in api._FTYPE_OF:
+        type_ = api._FTYPE_OF.get(k.dtype)
+        if type_ is None or v.dtype != k.dtype:
             raise ValueError("keys and values have to be of one float type")
-        k_strides, v_strides = self._lines(k, None, self.heads, "k"), self._lines(v, tokens, self.heads, "v")
-        at = self._indices(slots, torch.int64, (tokens,), "slots")
-        if tokens == 0:
-            return
-        api.check(self._lib.pbz_cache_append(self._h, self._ref, tokens, _Lines(k.data_ptr(), *k_strides),
-                                             _Lines(v.data_ptr(), *v_strides), api._ftype_of(k), at, api._stream()))
+        api.check(api._binding.cache_append(self._append, self._handle, self._at, self._held, type_, k, v, slots))
 
     def copy_pages(self, pairs) -> None:
         """pbz_cache_copy_pages: pairs [n, 2] (from, to), on the host."""
         pairs = np.ascontiguousarray(pairs, dtype=np.int32).reshape(-1, 2)
         if len(pairs):
-            api.check(self._lib.pbz_cache_copy_pages(self._h, self._ref, len(pairs), pairs.ctypes.data, api._stream()))
+            api.check(api._binding.cache_copy(self._copy, self._handle, self._at, pairs))
 
     def attend(self, q, table, lengths, starts=None, max_new: Optional[int] = None, max_length: int = 0,
                causal: bool = True, window: int = 0, scale: Optional[float] = None, out=None, lse=None, workspace=None):
@@ -225,48 +209,36 @@ class PagedCache:
         sequence's new tokens (None: one token a sequence).  max_new, max_length: the host's bounds of the runs of new
         tokens and of the lengths, by which the work is dealt out (defaults: all tokens; the table's width).
         lse: float32 [tokens, query heads], written.  scale: 1 / sqrt(head_dim) when None."""
-        torch = api._torch()
         if q.dim() != 3:
             raise ValueError("q has to be [tokens, query heads, head_dim]")
-        tokens, q_heads = q.shape[0], q.shape[1]
-        seqs = lengths.shape[0]
-        args = _Attention()
-        args.q_token_stride, args.q_head_stride = self._lines(q, None, q_heads, "q")
-        if table.dim() != 2 or table.dtype != torch.int32 or table.shape[0] != seqs or table.device != self.device or \
-                (table.shape[1] > 1 and table.stride(1) != 1):
-            raise ValueError(f"table has to be an int32 tensor [{seqs}, pages] with contiguous rows on the cache's device")
+        torch = api._torch()
         if out is None:
-            out = torch.empty((tokens, q_heads, self.head_dim), dtype=q.dtype, device=q.device)
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         elif out.dtype != q.dtype:
             raise ValueError("out has to be of q's type")
-        args.out_token_stride, args.out_head_stride = self._lines(out, tokens, q_heads, "out")
-        args.lengths = self._indices(lengths, torch.int32, (seqs,), "lengths")
-        if starts is not None:
-            args.starts = self._indices(starts, torch.int32, (seqs + 1,), "starts")
-        if lse is not None:
-            args.lse = self._indices(lse, torch.float32, (tokens, q_heads), "lse")
+        args = _Attention()
+        api._binding.cache_attention(args, self._held, q, out, lse, starts, lengths, table)
+        tokens = args.n_tokens
         if tokens == 0:
             return out
-        args.q, args.out, args.table = q.data_ptr(), out.data_ptr(), table.data_ptr()
-        args.type, args.q_heads = api._FTYPE_OF.get(q.dtype, -1), q_heads
-        args.n_tokens, args.n_seqs = tokens, seqs
-        args.table_stride, args.max_pages = max(table.stride(0), table.shape[1]), table.shape[1]
+        args.type = api._FTYPE_OF.get(q.dtype, -1)
         args.max_new = tokens if max_new is None else int(max_new)
         args.max_length, args.causal, args.window = int(max_length), 1 if causal else 0, int(window)
         args.scale = 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale)
-        stream = api._stream()
         if workspace is None:
-            sizes = (tokens, q_heads, seqs, args.max_pages, args.max_new, args.max_length, args.window, starts is None, args.type)
+            sizes = (tokens, args.q_heads, args.n_seqs, args.max_pages, args.max_new, args.max_length, args.window, starts is None, args.type)
             need = self._need.get(sizes)
             if need is None:
                 need = self.workspace_bytes(args)
                 if len(self._need) < 256:
                     self._need[sizes] = need
-            workspace = self._spaces.get(stream)
-            if workspace is None or workspace.numel() < need:
-                workspace = self._spaces[stream] = torch.empty(need, dtype=torch.uint8, device=self.device)
-        api.check(self._lib.pbz_cache_attend(self._h, self._ref, _c.byref(args), api._ptr(workspace),
-                                             workspace.numel() * workspace.element_size(), stream))
+            stream = api._stream()
+            workspace, room = self._spaces.get(stream, (None, 0))
+            if room < need:
+                workspace, room = self._spaces[stream] = torch.empty(need, dtype=torch.uint8, device=self.device), need
+        else:
+            room = workspace.numel() * workspace.element_size()
+        api.check(api._binding.cache_attend(self._attend, self._handle, self._at, args, workspace, room))
         return out
 
     def workspace_bytes(self, args: _Attention) -> int:
