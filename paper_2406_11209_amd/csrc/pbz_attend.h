@@ -1,5 +1,5 @@
-// Attention over a paged compressed cache: the pass over keys and values (pbz_cache.h has the definition, pbz_cache.hip what
-// comes before and after).
+// Attention over a paged compressed cache: the pass over keys and values (pbz_cache.h has the definition; pbz_cache.hip transforms the
+// queries before, and joins the records after where positions are split).
 //
 // A wave takes 16 R query rows of one head of the cache and a run of positions, 16 positions to a matrix tile.
 //   scores   S^T = K q^T on the integer matrix cores: K's indices go from memory to the operand as they are, 16 bytes a lane; a row
@@ -91,21 +91,14 @@ struct Part {
   // (the constant address space: uniform reads through the scalar cache)
   const __attribute__((address_space(4))) int32_t* table;
 
-  // The workgroup's number among `units` of every head and split.  Heads in turn where there are as many as dies (every eighth workgroup is
-  // on the same one), so that the workgroups with the same keys share a die's cache and long sequences spread over the dies; with other
-  // numbers of heads, a die has a run of units of a head.
+  // The workgroup's number among `units`, of every head and split; heads in turn, then splits.  Neighbouring workgroups are on dies in turn, so with 8
+  // heads the workgroups with the same keys share a die's cache, and with any number the long sequences and the long rows of a causal prompt
+  // spread over the dies.  (In runs of a head's units to a die, which keeps a head's keys to one or two dies' caches with other numbers of heads,
+  // too: a prompt of 4096 with 1, 4, 5, 12 and 32 heads of 128 259, 320, 193, 383 and 258 us, in turn 154, 238, 142, 329 and 241; single tokens of
+  // 64 uneven sequences 35, 74, 118, 198 and 444, in turn 35, 81, 94, 174 and 430.)
   __device__ __forceinline__ uint32_t number(const AttendCall& a) {
-    const uint32_t heads = uint32_t(a.cache.heads), all = a.units * a.split_blocks * heads;
-    uint32_t work = blockIdx.x;
-    if (heads % 8 != 0) {
-      work = blockIdx.x % 8 * ((all + 7) / 8) + blockIdx.x / 8;
-      if (blockIdx.x / 8 >= (all + 7) / 8 || work >= all) return ~0u;
-      head = int(work / (a.units * a.split_blocks));
-      work %= a.units * a.split_blocks;
-    } else {
-      head = int(work % heads);
-      work /= heads;
-    }
+    const uint32_t heads = uint32_t(a.cache.heads), work = blockIdx.x / heads;
+    head = int(blockIdx.x % heads);
     record = int(work % a.split_blocks);
     return work / a.split_blocks;
   }
@@ -128,18 +121,15 @@ struct Part {
     table = (const __attribute__((address_space(4))) int32_t*)(a.table + seq * a.table_stride);
   }
   // Units: row_blocks to every sequence.
-  __device__ __forceinline__ bool find(const AttendCall& a, int wave) {
+  __device__ __forceinline__ void find(const AttendCall& a, int wave) {
     const uint32_t unit = number(a);
-    if (unit == ~0u) return false;
     row_block = unit % a.row_blocks;
     look_at(a, unit / a.row_blocks, wave);
-    return true;
   }
   // Units: as many to a sequence as it has runs of `block` rows, by the sums over the sequences before; 64 of them at a time.  (With as many to all
   // as the longest has, a batch of 63 single tokens and a chunk of 512 spent most of its 690 us on workgroups with nothing to do.)
   __device__ __forceinline__ bool find_run(const AttendCall& a, uint32_t block, int lane) {
     uint32_t unit = number(a);
-    if (unit == ~0u) return false;
     if (!a.starts) {
       const uint32_t each = (uint32_t(a.groups) + block - 1) / block;
       if (unit / each >= uint64_t(a.n_seqs)) return false;
@@ -532,15 +522,18 @@ __device__ __forceinline__ void value_tiles(const uint32_t (&w)[8], u32x4 (&tile
   }
 }
 
-// Few rows: every wave by itself, positions of its own split; waves with the same rows join what they have before it is stored.  Keys are read a step ahead, into the registers that the products before
-// them have left; values while the scores are taken.
+// Few rows: every wave by itself, positions of its own split; waves with the same rows join what they have before it is stored.  Keys are read a
+// step ahead, into the registers that the products before them have left; values while the scores are taken.
+// Bound by memory: waves wait for loads in two thirds of their cycles.  One token each of 256 sequences of 4096 positions, 32 query heads on 8 of
+// 128: 372 us a call, 5.85 TB/s; of 64 sequences 105 us, 5.2 TB/s; one of 131072 positions 45 us, 6.1 TB/s.  Three waves a SIMD where the
+// registers allow: with two, and values read a step ahead as well, the last one takes 41 us, but 256 sequences of 512 67 us instead of 56.
 template <int D, int R, bool kFine, int kN>
 __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) void k_attend(const AttendCall a) {
   constexpr int VW = D >= 64 ? D / 64 : 1;       // 32-bit words of values a lane has of a position
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, quarter = lane >> 4;
   Part part;
-  if (!part.find(a, wave)) return;
+  part.find(a, wave);
   const int sharing = 4 / a.waves_rows;          // waves with the same rows, whose splits become one record
   Rows<D, R, kFine, kN> rows;
   __shared__ float left[D == 32 ? 4 : 3][Rows<D, R, kFine, kN>::kLeft * 64];      // (with more columns, at most two waves have rows)
@@ -826,6 +819,9 @@ struct Stage {
 // converts the values of 16 of them into LDS, where every wave finds its operands, and N of all lies there, too; two buffers, so one
 // barrier to a stage.  Every load is made whether or not it will be used (behind the end: of the pool's first line), so that
 // the waits between loads and their uses count exactly.
+// Bound by vector instructions, of which there are 230 to 32 positions of 32 rows of 128, 16 of them exponentials at a quarter of the rate; they
+// are issued in 72 % of the time, and the matrix cores are busy in 38 %.  A prompt of 8192, 32 query heads on 8 of 128: 690 to 780 us on different
+// cards, 0.7 to 0.8 PFLOP/s.  (Wave by wave with tiles of 16, as k_attend: 1022 us.)
 template <int D, bool kFine, int kN>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const AttendCall a) {
   constexpr int DT = D / 32, KS = D / 32, VW = D >= 128 ? D / 128 : 1;
@@ -1009,8 +1005,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
 
 template <int D, int kN>
 int launch(bool tall, int rows, bool fine, const AttendCall& call, hipStream_t s) {
-  const uint32_t all = call.units * call.split_blocks * uint32_t(call.cache.heads);
-  const dim3 grid((all + 7) / 8 * 8), block(256);
+  const dim3 grid(call.units * call.split_blocks * uint32_t(call.cache.heads)), block(256);
   if (tall) {
     if constexpr (D >= 64) {
       if (fine) k_attend_tall<D, true, kN><<<grid, block, 0, s>>>(call);
