@@ -381,9 +381,10 @@ int plan_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_attention*
   int64_t length = a->max_pages * cache->page_size;
   if (a->max_length > 0) length = std::min(length, a->max_length);
   if (a->window > 0) length = std::min(length, a->window + fresh + 63);
-  // Splits of the positions, where rows alone do not fill the chip: a chunk of 256 after 8192 takes 85 us with 1024 waves, 74 with 2048 and 89
-  // with 4096; the tall kernel for lines of 256 has one wave to a SIMD (32 rows after 16 x 4096: 155 us with 1024, 174 with 2048).  Down to
-  // 64 positions: one token after 8000 takes 18 us, 21 with at least 128 and 23 with 256.
+  // Splits of the positions, where rows alone do not fill the chip, for 1400, 2048 and 3000 waves: chunks of 10 to 387 after up to 3528 95, 87 and 107
+  // us, one token of 131072 71, 65 and 70, of 64 uneven sequences to 8200 128, 128 and 191; the tall kernel for lines of 256 has one wave to a SIMD
+  // (32 rows after 16 x 4096: 155 us with 1024, 174 with 2048).  Down to 64 positions: one token after 8000 takes 18 us, 21 with at least 128 and
+  // 23 with 256.
   // (max_new bounds the tiles of every sequence, all rows together those of all)
   const int64_t some = std::min(a->n_seqs * tiles, (a->n_tokens * groups + p->tile - 1) / p->tile + a->n_seqs);
   const int64_t alone = some * cache->heads, busy = p->tall && c->vol == 256 ? kBusyWaves / 2 : kBusyWaves;
