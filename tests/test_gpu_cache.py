@@ -213,6 +213,23 @@ def test_append_marks_lines_that_are_not_finite():
     assert bool(torch.isfinite(cache.k_N[0, 0, 3])) and bool(torch.isfinite(cache.v_N).all())
 
 
+@pytest.mark.parametrize("dim, transform", [(32, "dct"), (64, "haar"), (128, "dct"), (256, "dct")])
+def test_append_of_quotients_on_the_borders(dim, transform):
+    """127 C / N half-way between two indices, as near as FP64 comes: either of the two.  Next to that, by 2^-20 of a step, the nearer one."""
+    H = torch.from_numpy(matrix(transform, dim)).cuda()
+    k = torch.arange(dim, device="cuda", dtype=torch.float64) % 126
+    for away in (0.0, 2.0 ** -20, -2.0 ** -20):
+        C = (k + 0.5 + away) / 127.0
+        C[0] = 1.0                                                      # N
+        C = torch.stack([C, -C, 3.0 * C])[:, None]
+        cache = PagedCache(dim, 1, 1, 16, transform=transform)
+        cache.append(C @ H.t(), C @ H.t(), torch.arange(3, device="cuda"))
+        for F in (cache.k_F, cache.v_F):
+            r = 127.0 * C / C.abs().amax(-1, keepdim=True)
+            off = (F[0, 0, :3, None].double() - r).abs()
+            assert bool((off <= 0.5 + 1e-9).all()) and bool((F[0, 0, :3, 0].abs() == 127).all())
+
+
 # ---- attend ----------------------------------------------------------------------------------------------------------
 
 CASES = [
@@ -317,6 +334,59 @@ def test_rows_of_no_sequence_are_zero_beside_many_rows():
     assert bool((out[:11] == 0).all()) and bool((out[190:] == 0).all())
     assert bool((lse[:11] == -math.inf).all()) and bool((lse[190:] == -math.inf).all())
     check_attend(cache, q[11:190], out[11:190], lse[11:190], tables, [200, 100], [100, 79])
+
+
+# short enough for one workgroup to see every position of its rows, which then writes their results itself; row tiles to a workgroup 1, 2 and more
+SHORT = [
+    (32, 2, 4, 16, "f16", "f32", "haar", [100], [60], True, 0),
+    (32, 4, 3, 32, "bf16", "bf16", "dct", [64, 9, 0], [40, 9, 2], True, 0),
+    (64, 12, 2, 16, "bf16", "f32", "dct", [90, 250, 1], [20, 3, 1], True, 40),
+    (64, 1, 64, 64, "f16", "f16", "dct", [100], [1], True, 0),
+    (128, 16, 3, 16, "f16", "f32", "dct", [31, 200], [11, 13], False, 0),
+    (128, 4, 4, 64, "bf16", "f16", "haar", [250, 100, 17], [1, 4, 8], True, 0),
+    (256, 3, 8, 32, "bf16", "f32", "dct", [100, 40], [4, 1], True, 0),
+    (256, 1, 12, 16, "f16", "bf16", "haar", [60, 120], [1, 4], True, 33),
+]
+
+
+@pytest.mark.parametrize("case", SHORT, ids=[f"{i}" for i in range(len(SHORT))])
+def test_attend_short_sequences_of_few_rows(case):
+    dim, heads, groups, page, array, work, transform, lengths, counts, causal, window = case
+    cache = filled(PagedCache(dim, heads, sum(-(-n // page) for n in lengths) + 1, page, work, transform), 61)
+    tables, table, length_t = deal(cache, lengths, 62)
+    g = torch.Generator(device="cuda").manual_seed(63)
+    before, behind = 2, 3                                                # rows of no sequence
+    q = torch.randn(before + sum(counts) + behind, heads * groups, dim, generator=g, device="cuda").to(FLOATS[array])
+    out, lse = torch.full_like(q, 3.0), torch.full(q.shape[:2], 3.0, device="cuda")
+    cache.attend(q, table, length_t, starts=starts_of(counts) + before, max_new=max(counts), causal=causal, window=window, out=out, lse=lse)
+    own = slice(before, before + sum(counts))
+    check_attend(cache, q[own], out[own], lse[own], tables, lengths, counts, causal, window)
+    for rest in (slice(0, before), slice(before + sum(counts), None)):
+        assert bool((out[rest] == 0).all()) and bool((lse[rest] == -math.inf).all())
+
+
+def test_rows_of_no_sequence_are_zero_beside_split_positions():
+    cache = filled(PagedCache(128, 3, 60, 64), 64)
+    tables, table, lengths = deal(cache, [3000, 500], 65)
+    q = torch.randn(12, 6, 128, device="cuda").to(torch.bfloat16)
+    out, lse = torch.full_like(q, 3.0), torch.full(q.shape[:2], 3.0, device="cuda")
+    cache.attend(q, table, lengths, starts=torch.tensor([5, 6, 9], dtype=torch.int32, device="cuda"), max_new=3, out=out, lse=lse)
+    for rest in (slice(0, 5), slice(9, None)):
+        assert bool((out[rest] == 0).all()) and bool((lse[rest] == -math.inf).all())
+    check_attend(cache, q[5:9], out[5:9], lse[5:9], tables, [3000, 500], [1, 3])
+
+
+def test_queries_beyond_the_range_of_their_transform():
+    """A row whose coefficients overflow FP32 is not finite; its neighbours are what they are without it."""
+    cache = filled(PagedCache(128, 2, 4, 64), 66)
+    tables, table, lengths = deal(cache, [100, 130], 67)
+    q = torch.randn(2, 8, 128, device="cuda").to(torch.bfloat16)
+    q[0, 3] = 3e38
+    out = cache.attend(q, table, lengths)
+    assert not bool(torch.isfinite(out[0, 3].float()).any())
+    q[0, 3] = 0
+    assert torch.equal(cache.attend(q, table, lengths)[0, [0, 1, 2, 4, 5, 6, 7]], out[0, [0, 1, 2, 4, 5, 6, 7]])
+    assert torch.equal(cache.attend(q, table, lengths)[1], out[1])
 
 
 def test_values_that_widen_late():
