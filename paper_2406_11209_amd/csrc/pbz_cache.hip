@@ -11,7 +11,8 @@ namespace {
 
 constexpr int kMaxSplits = 256;
 constexpr int64_t kBusyWaves = 2048;         // waves that keep the chip busy: two to a SIMD
-constexpr int kPairsPerLaunch = 448;          // 3.5 KiB of a launch's 4 KiB of arguments
+// Pairs of pages to a launch: 3.5 KiB of its 4 KiB of arguments; twice as many where 16 bits hold a page's number.
+constexpr int kPairsPerLaunch = 448;
 
 // ---- append ----------------------------------------------------------------------------------------------------------
 
@@ -81,17 +82,19 @@ __global__ __launch_bounds__(256) void k_append(const AppendCall a) {
 
 constexpr int kPiece = 16384;      // bytes of a page's part to a workgroup
 
+template <typename Page, int kPairs>
 struct CopyCall {
   char* pool[4];
   int64_t bytes[4];            // of a page's part; a multiple of 16
   int32_t pieces[4];           // of a page, up to and with this part
-  int32_t pairs[2 * kPairsPerLaunch];
+  Page pairs[2 * kPairs];
 };
 
-// Bound by memory, and by the ramp and the end of each launch: 2048 pages of 64 tokens of 8 heads of 128 137 us in five launches, 4.0 TB/s (pieces of
-// 8 KiB 143, of 32 KiB 161).
+// Bound by memory, and by the ramp and the end of each launch: 2048 pages of 64 tokens of 8 heads of 128 126 us in three launches of 16-bit page
+// numbers, 4.4 TB/s, 137 us in five of 32-bit ones (and with these in pieces of 8 KiB 143, of 32 KiB 161).
 // The pairs travel with the launch: no copy to the device, nothing to keep alive, and a captured graph holds them.
-__global__ __launch_bounds__(256) void k_copy_pages(const CopyCall a) {
+template <typename Page, int kPairs>
+__global__ __launch_bounds__(256) void k_copy_pages(const CopyCall<Page, kPairs> a) {
   const int64_t from = a.pairs[2 * blockIdx.y], to = a.pairs[2 * blockIdx.y + 1];
   const int x = int(blockIdx.x);
   const int part = (x >= a.pieces[0]) + (x >= a.pieces[1]) + (x >= a.pieces[2]);
@@ -408,6 +411,29 @@ int plan_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_attention*
   return PBZ_OK;
 }
 
+// As many launches as the pairs need
+template <typename Page, int kPairs>
+int copy_pages(const pbz_codec* c, const pbz_cache* cache, int64_t n_pairs, const int32_t* pairs, hipStream_t stream) {
+  CopyCall<Page, kPairs> call;
+  const int64_t lines = int64_t(cache->heads) * cache->page_size;
+  void* const pools[4] = {cache->k_F, cache->v_F, cache->k_N, cache->v_N};
+  int64_t pieces = 0;
+  for (int i = 0; i < 4; ++i) {
+    call.pool[i] = static_cast<char*>(pools[i]);
+    call.bytes[i] = lines * (i < 2 ? c->vol : ftype_bytes(c->ftype));
+    pieces += (call.bytes[i] + kPiece - 1) / kPiece;
+    call.pieces[i] = int32_t(pieces);
+  }
+  for (int64_t at = 0; at < n_pairs; at += kPairs) {
+    const int64_t n = std::min<int64_t>(kPairs, n_pairs - at);
+    std::copy(pairs + 2 * at, pairs + 2 * (at + n), call.pairs);
+    k_copy_pages<Page, kPairs><<<dim3(unsigned(pieces), unsigned(n)), 256, 0, stream>>>(call);
+    const int st = hip_status(hipGetLastError());
+    if (st != PBZ_OK) return st;
+  }
+  return PBZ_OK;
+}
+
 }  // namespace
 }  // namespace pbz
 
@@ -479,24 +505,9 @@ int pbz_cache_copy_pages(const pbz_codec* c, const pbz_cache* cache, int64_t n_p
       return PBZ_ERR_ALLOC;
     }
   }
-  CopyCall call;
-  const int64_t lines = int64_t(cache->heads) * cache->page_size;
-  void* const pools[4] = {cache->k_F, cache->v_F, cache->k_N, cache->v_N};
-  int64_t pieces = 0;
-  for (int i = 0; i < 4; ++i) {
-    call.pool[i] = static_cast<char*>(pools[i]);
-    call.bytes[i] = lines * (i < 2 ? c->vol : ftype_bytes(c->ftype));
-    pieces += (call.bytes[i] + kPiece - 1) / kPiece;
-    call.pieces[i] = int32_t(pieces);
-  }
-  for (int64_t at = 0; at < n_pairs; at += kPairsPerLaunch) {
-    const int64_t n = std::min<int64_t>(kPairsPerLaunch, n_pairs - at);
-    std::copy(pairs + 2 * at, pairs + 2 * (at + n), call.pairs);
-    k_copy_pages<<<dim3(unsigned(pieces), unsigned(n)), 256, 0, static_cast<hipStream_t>(stream)>>>(call);
-    const int launched = hip_status(hipGetLastError());
-    if (launched != PBZ_OK) return launched;
-  }
-  return PBZ_OK;
+  const auto stream_ = static_cast<hipStream_t>(stream);
+  if (cache->n_pages <= 65536) return copy_pages<uint16_t, 2 * kPairsPerLaunch>(c, cache, n_pairs, pairs, stream_);
+  return copy_pages<int32_t, kPairsPerLaunch>(c, cache, n_pairs, pairs, stream_);
 }
 
 int pbz_cache_attend_workspace(const pbz_codec* c, const pbz_cache* cache, const pbz_attention* a, size_t* bytes) {

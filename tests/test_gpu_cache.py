@@ -536,6 +536,22 @@ def test_copy_pages(dim, heads, page, work, pairs):
         assert torch.equal(got, w)
 
 
+@pytest.mark.parametrize("n_pages, n_pairs", [(65536, 897), (65537, 449), (65600, 3)])
+def test_copy_pages_of_pools_of_many_pages(n_pages, n_pairs):
+    """Pages' numbers of 16 bits and of more, in more pairs than a launch takes."""
+    cache = filled(PagedCache(32, 1, n_pages, 16, "f16"), 71)
+    order = np.random.default_rng(72).permutation(n_pages)[:2 * n_pairs].astype(np.int32)
+    order[order == n_pages - 1] = order[0]
+    order[0] = n_pages - 1
+    pairs = order.reshape(-1, 2)
+    want = [p.clone() for p in cache.pools]
+    for pool in want:
+        pool[torch.from_numpy(pairs[:, 1].copy()).cuda().long()] = pool[torch.from_numpy(pairs[:, 0].copy()).cuda().long()]
+    cache.copy_pages(pairs)
+    for pool, expected in zip(cache.pools, want):
+        assert torch.equal(pool, expected)
+
+
 def test_sequences_forked_written_and_compacted():
     """Sequences as a program uses them, against the lines kept aside in plain tensors."""
     cache = PagedCache(64, 2, 40, 16, "f32")
