@@ -10,8 +10,8 @@
 //            which the wave votes on, so the usual tile exchanges nothing.  The sums stay per lane to the end.
 //   values   O^T += V^T P^T in FP16 with FP32 sums: the weights, times N over the largest N so far (a power of two) and 2^7, are in
 //            the registers where the product wants them (the order of positions within a product is free, as long as both operands
-//            have the same); the largest is 2^15, and what is 2^-29 of it is still a normal FP16 number.  V's bytes become FP16 integers
-//            by permutes: 0x6400 | (F + 128) is 1024 + 128 + F, minus 1152.
+//            have the same); the largest is 2^15, and what is 2^-29 of it is still a normal FP16 number.  V's bytes become FP16 by a
+//            permute and a multiply-add of two.
 // Lanes 16 apart share a position's line: a line of 128 is one 128-byte read of 8 (keys) or 16 lanes (values).
 #pragma once
 
@@ -73,12 +73,14 @@ __device__ __forceinline__ void load_values(const int8_t* p, uint32_t (&w)[D >= 
   }
 }
 
-// bytes kPair and kPair + 1 (both biased by 128) as FP16 integers
-template <int kPair>
-__device__ __forceinline__ uint32_t two_values(uint32_t bytes) {
-  const uint32_t biased = __builtin_amdgcn_perm(bytes, 0x64646464u, kPair == 0 ? 0x00050004u : 0x00070006u);
-  const f16x2 v = __builtin_bit_cast(f16x2, biased) - f16x2{_Float16(1152), _Float16(1152)};
-  return __builtin_bit_cast(uint32_t, v);
+// Byte kByte of two words, biased by 128, as FP16: the bias off, and over 2^9.  A byte by itself is an FP16 subnormal, F + 128 times 2^-24; the
+// product with 2^15, minus 128 times 2^-9, is exact.
+constexpr float kValueUnit = 512.f;
+template <int kByte>
+__device__ __forceinline__ uint32_t two_values(uint32_t w0, uint32_t w1) {
+  const f16x2 biased = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(w1, w0, 0x0c000c00u | ((4u + kByte) << 16) | kByte));
+  const _Float16 up = _Float16(32768.f), down = _Float16(-0.25f);
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(biased, f16x2{up, up}, f16x2{down, down}));
 }
 
 // What a workgroup works on: a sequence's rows and positions, cut to what the arrays have, and a head of the cache.
@@ -433,7 +435,7 @@ struct Rows {
   // What a wave leaves for another with the same rows: per lane references, totals, sums in one unit; the lanes of a wave side by side.
   static constexpr int kLeft = R * (2 + 4 * DT);
   __device__ __forceinline__ void leave(float* left, int lane) const {
-    const float unit = widest * (1.f / (128.f * 127.f));
+    const float unit = widest * (kValueUnit / (128.f * 127.f));
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       left[(2 * r) * 64 + lane] = top[r];
@@ -445,7 +447,7 @@ struct Rows {
     }
   }
   __device__ __forceinline__ void into_unit() {
-    const float unit = widest * (1.f / (128.f * 127.f));
+    const float unit = widest * (kValueUnit / (128.f * 127.f));
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -514,11 +516,10 @@ __device__ __forceinline__ void value_tiles(const uint32_t (&w)[8], u32x4 (&tile
 #pragma unroll
   for (int pair = 0; pair < 4; ++pair) {
     const uint32_t w0 = w[2 * pair] ^ 0x80808080u, w1 = w[2 * pair + 1] ^ 0x80808080u;
-    const uint32_t lo = __builtin_amdgcn_perm(w1, w0, 0x05010400u), hi = __builtin_amdgcn_perm(w1, w0, 0x07030602u);
-    tiles[0][pair] = two_values<0>(lo);
-    tiles[1][pair] = two_values<1>(lo);
-    tiles[2][pair] = two_values<0>(hi);
-    tiles[3][pair] = two_values<1>(hi);
+    tiles[0][pair] = two_values<0>(w0, w1);
+    tiles[1][pair] = two_values<1>(w0, w1);
+    tiles[2][pair] = two_values<2>(w0, w1);
+    tiles[3][pair] = two_values<3>(w0, w1);
   }
 }
 
@@ -739,7 +740,7 @@ struct TallRows {
   __device__ __forceinline__ void store(const AttendCall& a, const Part& part, uint32_t first_row, float* staged, int c, int half) {
     const float l = total + __shfl_xor(total, 32);
     const float top = l != l ? 0.f : -minus_top;         // a row that sees a NaN is one, also where it sees nothing else
-    const float unit = widest * (1.f / (128.f * 127.f));
+    const float unit = widest * (kValueUnit / (128.f * 127.f));
     const bool there = first_row + c < part.rows;
     const uint32_t row = there ? first_row + c : part.rows - 1, token = row / uint32_t(a.groups);
     const int64_t place = (part.first + token) * a.q_heads + int64_t(part.head) * a.groups + (row - token * uint32_t(a.groups));
@@ -819,7 +820,7 @@ struct Stage {
 // converts the values of 16 of them into LDS, where every wave finds its operands, and N of all lies there, too; two buffers, so one
 // barrier to a stage.  Every load is made whether or not it will be used (behind the end: of the pool's first line), so that
 // the waits between loads and their uses count exactly.
-// Bound by vector instructions, of which there are 230 to 32 positions of 32 rows of 128, 16 of them exponentials at a quarter of the rate; they
+// Bound by vector instructions, of which there are 220 to 32 positions of 32 rows of 128, 16 of them exponentials at a quarter of the rate; they
 // are issued in 72 % of the time, and the matrix cores are busy in 38 %.  A prompt of 8192, 32 query heads on 8 of 128: 690 to 780 us on different
 // cards, 0.7 to 0.8 PFLOP/s.  (Wave by wave with tiles of 16, as k_attend: 1022 us.)
 template <int D, bool kFine, int kN>
