@@ -821,7 +821,7 @@ struct Stage {
 // barrier to a stage.  Every load is made whether or not it will be used (behind the end: of the pool's first line), so that
 // the waits between loads and their uses count exactly.
 // Bound by vector instructions, of which there are 220 to 32 positions of 32 rows of 128, 16 of them exponentials at a quarter of the rate; they
-// are issued in 72 % of the time, and the matrix cores are busy in 38 %.  A prompt of 8192, 32 query heads on 8 of 128: 690 to 780 us on different
+// are issued in 71 % of the time, and the matrix cores are busy in 38 %.  A prompt of 8192, 32 query heads on 8 of 128: 690 to 780 us on different
 // cards, 0.7 to 0.8 PFLOP/s.  (Wave by wave with tiles of 16, as k_attend: 1022 us.)
 template <int D, bool kFine, int kN>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const AttendCall a) {

@@ -1,5 +1,5 @@
 // The paged compressed cache (pbz_cache.h): checks and launches, the kernels that append lines and copy pages, and what an
-// attention call does before and after its pass over keys and values (pbz_attend.hip).
+// attention call does before and after its pass over keys and values (pbz_attend.h).
 #include <algorithm>
 #include <cmath>
 #include <vector>

@@ -15,8 +15,8 @@
 // (With selects between sums and differences, and the orthonormal factors at every step: FP64 as 9 instructions a value and split and 9 a value
 // and sum, 4 and 4 now.)
 // 16 values to a lane: with 32, one split less, but an in-register transform of 341 multiply-adds instead of 85 and twice the code, which a
-// launch over few lines fetches for nearly as long as it computes (128 keys and values of 64 tokens: 9.2 us, 6.7 with 16; over many lines the two
-// are the same).
+// launch over few lines fetches for nearly as long as it computes (keys and values of 64 tokens, before the splits were as they are: 9.2 us, 6.7 with
+// 16; over many lines the two were the same).
 //
 // Haar: 16 values within a lane, then the lanes' sums among each other.
 #pragma once
