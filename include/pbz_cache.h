@@ -67,12 +67,14 @@ int pbz_cache_copy_pages(const pbz_codec* codec, const pbz_cache* cache, int64_t
  * 0 <= j < lengths[b]; a row that sees nothing is zero, its lse -infinity.  Rows of no sequence are zero, too.
  * Query head g reads the cache's head g / (q_heads / heads).
  * What is outside its bounds is not read: table entries outside the pool hide their positions, lengths beyond the table
- * are cut to it, starts to n_tokens.  Hidden positions' contents, whatever they are, do not reach the result (a finite N that
- * other rows see may choose the power of two by which weights are scaled before they are rounded, no more); a line with
- * an N that is not finite makes the rows that see it not finite.
+ * are cut to it, starts to n_tokens.  Hidden positions' contents, whatever they are, do not reach the result (but for the
+ * order of FP32 roundings: what weights refer to is renewed for several rows at a time); a line with an N that is not
+ * finite makes the rows that see it not finite.
  * Arithmetic: a query row is transformed in FP32 and held in 16-bit fixed point relative to its largest coefficient;
  * products with F are exact in integers; scores, running maxima and sums, and the output's sums are FP32; a weight
- * (times N) is rounded to FP16 once, or held in two FP16 parts where q and out are FP16. */
+ * (times N) is rounded to FP16 once, or held in two FP16 parts where q and out are FP16.  The unit of that is a power of
+ * two, such that a row's largest weight times N is between 1 and 2^15 (above 2^-79, where another row's N is 2^24 or
+ * more): what is smaller than 2^-14 of the former is off by 2^-25 of it. */
 typedef struct pbz_attention {
   const void* q;               /* device, element (t, g, d) at t * q_token_stride + g * q_head_stride + d */
   void* out;                   /* device, likewise; must not overlap q */

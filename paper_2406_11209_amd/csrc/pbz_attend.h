@@ -12,6 +12,10 @@
 //            the registers where the product wants them (the order of positions within a product is free, as long as both operands
 //            have the same); the largest is 2^15, and what is 2^-29 of it is still a normal FP16 number.  V's bytes become FP16 by a
 //            permute and a multiply-add of two.
+//   range    The largest N so far may be of a line that a row does not see, or sees with no weight, and then all of its weights would be
+//            lost in FP16.  So it is checked that each row has a weight of 1 at least, where the references or the largest N change, which is
+//            seldom.  While some row has none, the rows' largest weights are found at every step, and such rows have a factor of their own, a
+//            power of two.  The check costs a prompt 0.5 % (712 -> 715 us), a single token of 300 positions 6 % (10.9 -> 11.6 us).
 // Lanes 16 apart share a position's line: a line of 128 is one 128-byte read of 8 (keys) or 16 lanes (values).
 #pragma once
 
@@ -30,6 +34,22 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kSlack = 8.f;          // by how much (in log2) a score may pass the maximum that the weights refer to
+
+// N of values is taken relative to the next power of two of the largest so far, between these: what a row's own factor does not reach (below) is then
+// 2^-79 and less, whatever N other rows see.
+constexpr uint32_t kLeastWide = 0x33800000u, kMostWide = 0x4b800000u;      // 2^-24, 2^24
+__device__ __forceinline__ float wide_unit(float wide) {
+  const uint32_t up = (__float_as_uint(wide) + 0x7fffffu) & 0x7f800000u;
+  return __uint_as_float(up > kMostWide ? kMostWide : up < kLeastWide ? kLeastWide : up);
+}
+
+// The exponent of a row's own factor, by its largest weight so far (or less): none from 1 to 2^15, where what is below FP16's normal numbers is off by
+// 2^-25 of the largest at most.  Otherwise the largest becomes 2^10.
+__device__ __forceinline__ int fitting(float largest) {
+  if (largest == 0.f || (largest >= 1.f && largest <= 32768.f)) return 0;
+  const int up = 10 + 127 - int(__float_as_uint(largest) >> 23);
+  return up > 96 ? 96 : up;
+}
 
 // N of four neighbouring positions, as stored
 template <int kN> struct Scales { using Raw = uint2; };
@@ -273,12 +293,12 @@ struct Rows {
   int low[R], high[R];                                   // positions that a row sees
   i32x4 q_high[R][KS], q_low[R][KS];
   float q_scale[R];
-  float top[R], reference[R], total[R];
+  float top[R], reference[R], total[R];                  // reference: of weights and total, the top but for the row's own factor
   f32x4 sum[R][DT];
   float widest, narrow;      // the largest N of the values so far (rounded up to a power of two); 2^7 over it
   f16x8 p[R], p_low[R];      // weights of a step
 
-  __device__ __forceinline__ void begin(const AttendCall& a, const Part& part, uint32_t first_row, int c, int quarter) {
+  __device__ __forceinline__ void begin(const AttendCall& a, const Part& part, uint32_t first_row, int c, int quarter, float* largest) {
     const uint32_t groups = uint32_t(a.groups);
     const int before = part.length - part.fresh;
 #pragma unroll
@@ -305,6 +325,7 @@ struct Rows {
       top[r] = kNegInf;
       reference[r] = 0.f;
       total[r] = 0.f;
+      largest[64 * r] = 0.f;
 #pragma unroll
       for (int t = 0; t < DT; ++t) sum[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -329,20 +350,16 @@ struct Rows {
     }
   }
 
-  // what the weights refer to grows; seldom
-  __device__ __forceinline__ void grow(const f32x4 (&N)[2], const float (&most)[R]) {
+  // What the weights refer to grows; seldom.  largest: in LDS, 64 apart, the largest weights so far, or less; of a lane's positions, and while some
+  // row is unfit, of all the row's.
+  __device__ __forceinline__ void grow(const f32x4 (&N)[2], const float (&most)[R], float* largest, bool unfit) {
     float wide = 0.f;                        // of what is finite
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) wide = fmaxf(wide, fabsf(N[u][i]) < __builtin_huge_valf() ? fabsf(N[u][i]) : 0.f);
     for (int apart = 1; apart < 64; apart <<= 1) wide = fmaxf(wide, __shfl_xor(wide, apart));
-    float wider = widest;
-    if (wide > widest) {
-      // the next power of two, within the range whose reciprocal is a normal number
-      const uint32_t up = (__float_as_uint(wide) + 0x7fffffu) & 0x7f800000u;
-      wider = __uint_as_float(up > 0x7e000000u ? 0x7e000000u : up < 0x04000000u ? 0x04000000u : up);
-    }
+    const float wider = wide > widest ? wide_unit(wide) : widest;
     const float shrink = wider > 0.f ? widest / wider : 1.f;
     widest = wider;
     narrow = wider > 0.f ? 128.f / wider : 0.f;
@@ -352,16 +369,68 @@ struct Rows {
       m = fmaxf(m, __shfl_xor(m, 16));
       m = fmaxf(m, __shfl_xor(m, 32));
       const float factor = m == kNegInf ? 1.f : __builtin_amdgcn_exp2f(top[r] - m);
+      const float had = largest[64 * r], has = had * factor * shrink;
+      const int now = unfit ? fitting(has) : 0;
+      const float by = __builtin_amdgcn_ldexpf(factor, unfit ? now - fitting(had) : 0);
       top[r] = m;
-      reference[r] = m == kNegInf ? 0.f : m;
-      total[r] *= factor;
+      reference[r] = m == kNegInf ? 0.f : m - float(now);
+      largest[64 * r] = has;
+      total[r] *= by;
 #pragma unroll
-      for (int t = 0; t < DT; ++t) sum[r][t] *= factor * shrink;
+      for (int t = 0; t < DT; ++t) sum[r][t] *= by * shrink;
     }
   }
 
+  // Rows that see something, and among whose positions none has a weight that is surely large enough; and whether one may be too large
+  __device__ __forceinline__ bool wanting(int r, float most) const {
+    const uint64_t fits = __ballot(most >= 1.f), seeing = __ballot(place[r] >= 0 && top[r] != kNegInf);
+    return ((seeing & ~(fits | (fits >> 16) | (fits >> 32) | (fits >> 48)) & 0xffffu) | __ballot(most > 32768.f)) != 0;
+  }
+  // a lane's largest weight of a step; N: over the largest so far and times 2^7
+  __device__ __forceinline__ float largest_of(int r, const float (&x)[R][2][4], const f32x4 (&N)[2]) const {
+    float most = 0.f, minus = top[r] == kNegInf ? 0.f : -top[r];
+    asm volatile("" : "+v"(minus));              // otherwise the exponentials are kept for the usual steps' use, in registers that those want
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(__builtin_amdgcn_exp2f(fmaf(x[r][u][i], q_scale[r], minus)) * N[u][i]));
+    return place[r] < 0 ? 0.f : most;
+  }
+  // After a change of what weights refer to, and while some row is unfit: whether one is.  Has a factor of its own, or may need one, that is.
+  __device__ __forceinline__ bool fit(const float (&x)[R][2][4], const f32x4 (&N)[2], float* largest, bool unfit) {
+    float most[R];
+    bool any = unfit;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      most[r] = fmaxf(largest[64 * r], largest_of(r, x, N));
+      any = any || wanting(r, most[r]);
+    }
+    if (__builtin_expect(!any, 1)) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) largest[64 * r] = most[r];
+      return false;
+    }
+    bool own = false;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float m = most[r];
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      const float had = unfit ? largest[64 * r] : 0.f, has = m < __builtin_huge_valf() ? m : had;      // (infinite: so is the row's result)
+      largest[64 * r] = has;
+      const int now = fitting(has);
+      const float by = __builtin_amdgcn_ldexpf(1.f, now - fitting(had));
+      if (top[r] != kNegInf) reference[r] = top[r] - float(now);
+      total[r] *= by;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) sum[r][t] *= by;
+      // (a row that has seen nothing but N of zero may come to need a factor without its reference changing)
+      own = own || now != 0 || (has == 0.f && top[r] != kNegInf && place[r] >= 0);
+    }
+    return __any(own);
+  }
   // Scores to weights, of 32 positions.  whole: all of them are there, and every row sees them.
-  __device__ __forceinline__ void weigh(float (&x)[R][2][4], f32x4 (&N)[2], int at, bool whole, int there0, int there1, int quarter) {
+  __device__ __forceinline__ void weigh(float (&x)[R][2][4], f32x4 (&N)[2], int at, bool whole, int there0, int there1, int quarter, float* largest, bool& unfit) {
     bool odd = false;
     if (!whole) {
 #pragma unroll
@@ -395,17 +464,19 @@ struct Rows {
       most[r] *= q_scale[r];
       more = more || most[r] > top[r] + kSlack;
     }
-    if (__any(more)) grow(N, most);
+    const bool grown = __any(more);
+    if (grown) grow(N, most, largest, unfit);
+    const f32x4 n[2] = {N[0] * narrow, N[1] * narrow};
+    if (grown || unfit) unfit = fit(x, n, largest, unfit);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const f32x4 n = N[u] * narrow;
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float e = __builtin_amdgcn_exp2f(fmaf(x[r][u][i], q_scale[r], -reference[r]));
           total[r] += e;
-          const float w = e * n[i];
+          const float w = e * n[u][i];
           const _Float16 h = _Float16(w);
           p[r][u * 4 + i] = h;
           if constexpr (kFine) p_low[r][u * 4 + i] = _Float16(w - float(h));
@@ -434,24 +505,29 @@ struct Rows {
 
   // What a wave leaves for another with the same rows: per lane references, totals, sums in one unit; the lanes of a wave side by side.
   static constexpr int kLeft = R * (2 + 4 * DT);
-  __device__ __forceinline__ void leave(float* left, int lane) const {
-    const float unit = widest * (kValueUnit / (128.f * 127.f));
+  __device__ __forceinline__ float unit_of(int r, const float* largest, bool unfit) const {
+    return __builtin_amdgcn_ldexpf(widest * (kValueUnit / (128.f * 127.f)), unfit ? -fitting(largest[64 * r]) : 0);
+  }
+  __device__ __forceinline__ void leave(float* left, int lane, const float* largest, bool unfit) const {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
+      const float unit = unit_of(r, largest, unfit);
       left[(2 * r) * 64 + lane] = top[r];
-      left[(2 * r + 1) * 64 + lane] = total[r];
+      left[(2 * r + 1) * 64 + lane] = __builtin_amdgcn_ldexpf(total[r], unfit ? -fitting(largest[64 * r]) : 0);
 #pragma unroll
       for (int t = 0; t < DT; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) left[(2 * R + (r * DT + t) * 4 + i) * 64 + lane] = sum[r][t][i] * unit;
     }
   }
-  __device__ __forceinline__ void into_unit() {
-    const float unit = widest * (kValueUnit / (128.f * 127.f));
+  __device__ __forceinline__ void into_unit(const float* largest, bool unfit) {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) {
+      const float unit = unit_of(r, largest, unfit);
+      total[r] = __builtin_amdgcn_ldexpf(total[r], unfit ? -fitting(largest[64 * r]) : 0);
 #pragma unroll
       for (int t = 0; t < DT; ++t) sum[r][t] *= unit;
+    }
   }
   __device__ __forceinline__ void take(const float* left, int lane) {
 #pragma unroll
@@ -538,12 +614,14 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
   const int sharing = 4 / a.waves_rows;          // waves with the same rows, whose splits become one record
   Rows<D, R, kFine, kN> rows;
   __shared__ float left[D == 32 ? 4 : 3][Rows<D, R, kFine, kN>::kLeft * 64];      // (with more columns, at most two waves have rows)
+  __shared__ float largest[4][R * 64];
   if (a.records == 1 && a.starts && part.seq == 0 && part.row_block == 0) zero_rest(a, part.head, D);
   const uint32_t together = uint32_t(a.waves_rows) * (16 * R);
   for (uint32_t base = part.row_block * together; base < part.rows; base += a.row_blocks * together) {
     const uint32_t first = base + uint32_t(wave % a.waves_rows) * (16 * R);
     const bool any = first < part.rows;
-    rows.begin(a, part, first, c, quarter);
+    rows.begin(a, part, first, c, quarter, largest[wave] + lane);
+    bool unfit = false;                          // some row's weights have a factor of its own, or may need one
     const Range sees(a, part, any ? first : base, any && part.rows - first < 16 * R ? part.rows - first : any ? 16 * R : 1);
     const int64_t start = (sees.from & ~63) + int64_t(part.split) * a.chunk;
     const int begin = start < sees.to ? int(start) : sees.to;
@@ -583,7 +661,7 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
         if (at + 32 < end) key[u].load(a, next[u].line, c, quarter);
       }
       const bool whole = at >= sees.all_from && at + 32 <= sees.all_to && now[0].there == 16 && now[1].there == 16;
-      rows.weigh(x, N, at, whole, now[0].there, now[1].there, quarter);
+      rows.weigh(x, N, at, whole, now[0].there, now[1].there, quarter, largest[wave] + lane, unfit);
 #pragma unroll
       for (int h = 0; h < VW; ++h) {
         u32x4 tiles[4];
@@ -596,11 +674,11 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
     }
     const int turn = wave / a.waves_rows;
     if (sharing > 1) {
-      if (turn > 0) rows.leave(left[wave - a.waves_rows], lane);
+      if (turn > 0) rows.leave(left[wave - a.waves_rows], lane, largest[wave] + lane, unfit);
       __syncthreads();
     }
     if (turn == 0) {
-      rows.into_unit();
+      rows.into_unit(largest[wave] + lane, unfit);
       for (int w = 1; w < sharing; ++w) rows.take(left[wave + (w - 1) * a.waves_rows], lane);
       wave_lds_sync();
       const int at_end = this_lane();
@@ -609,6 +687,12 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
     if (sharing > 1) __syncthreads();
   }
 }
+
+// In LDS: the largest weight so far of a lane's positions, or less, and the exponent of the row's own factor.
+struct Fitting {
+  float largest;
+  int own;
+};
 
 // A wave's 32 rows of one head in tiles of 32: the same as Rows, a lane having one row and 16 of a step's 32 positions,
 // 8 (i / 4) + 4 half + i % 4.  Whether the weights' reference has to grow shows in their sum, which is taken anyway: a lane's part of it
@@ -622,7 +706,8 @@ struct TallRows {
   f32x16 sum[DT];
   f16x8 p[2], p_low[2];
 
-  __device__ __forceinline__ void begin(const AttendCall& a, const Part& part, uint32_t first_row, int c, int half) {
+  __device__ __forceinline__ void begin(const AttendCall& a, const Part& part, uint32_t first_row, int c, int half, Fitting* fitted) {
+    fitted->largest = 0.f;
     const uint32_t groups = uint32_t(a.groups);
     const uint32_t asked = first_row + c;
     const bool there = asked < part.rows;
@@ -661,12 +746,39 @@ struct TallRows {
     for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(key[s], q_low[s], acc, 0, 0, 0);
   }
 
-  // the values' largest N so far is another one, by whose share the sums shrink
-  __device__ __forceinline__ void widen(float wider) {
-    const float shrink = widest / wider;
-    widest = wider;
+  // After a change of what weights refer to, by which the sums change, and while some row is unfit (as in Rows): whether one is.  e is brought to
+  // where FP16 can hold what becomes of it.  beyond: some N is more than 2^7.
+  __device__ __forceinline__ bool wanting(float most) const {
+    const uint64_t fits = __ballot(most >= 1.f), seeing = __ballot(high >= 0 && minus_top != -kNegInf);
+    return (seeing & ~(fits | (fits >> 32)) & 0xffffffffu) != 0;
+  }
+  __device__ __forceinline__ bool fit(float (&e)[16], const f32x4 (&N)[4], float by, bool beyond, Fitting* fitted, bool unfit) {
+    float most = fitted->largest * by;
+    int before = 0, now = 0;
+    bool rows = unfit || beyond || wanting(most);
+    if (rows) {
 #pragma unroll
-    for (int t = 0; t < DT; ++t) sum[t] *= shrink;
+      for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(e[i] * N[i / 4][i % 4]));
+      rows = unfit || beyond || wanting(most);
+    }
+    if (__builtin_expect(rows, 0)) {
+      const bool seeing = high >= 0 && minus_top != -kNegInf;
+      before = unfit ? fitted->own : 0;
+      most = fmaxf(most, __shfl_xor(most, 32));
+      most = seeing && most < __builtin_huge_valf() ? most : 0.f;                  // (infinite: so is the row's result)
+      now = fitting(most);
+      fitted->own = now;
+      const float own = __builtin_amdgcn_ldexpf(1.f, now);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) e[i] *= own;
+      // (a row that has seen nothing but N of zero may come to need a factor without its reference changing)
+      rows = beyond || __any(now != 0 || (most == 0.f && seeing));
+    }
+    fitted->largest = most;
+    by = __builtin_amdgcn_ldexpf(by, now - before);
+#pragma unroll
+    for (int t = 0; t < DT; ++t) sum[t] *= by;
+    return rows;
   }
 
   // exponentials against the reference; their sum
@@ -693,8 +805,10 @@ struct TallRows {
       }
     }
   }
-  // e: the exponentials against the reference; more: their sum.  Where that does not do, a new reference and exponentials against that.
-  __device__ __forceinline__ void refer(const float (&x)[16], float (&e)[16], float more) {
+  // e: the exponentials against the reference; more: their sum.  Where that does not do, a new reference and exponentials against that;
+  // by: what the sums have to be multiplied by.
+  __device__ __forceinline__ bool refer(const float (&x)[16], float (&e)[16], float& more, const f32x4 (&N)[4], float by, bool beyond, Fitting* fitted,
+                                        bool unfit) {
     if (__any(!(more <= 256.f))) {
       float most = x[0];
 #pragma unroll
@@ -705,11 +819,10 @@ struct TallRows {
       const float factor = most == kNegInf ? 1.f : __builtin_amdgcn_exp2f(-minus_top - most);
       minus_top = -most;
       total *= factor;
-#pragma unroll
-      for (int t = 0; t < DT; ++t) sum[t] *= factor;
+      by *= factor;
       more = exponentials(x, most == kNegInf ? 0.f : minus_top, e);
     }
-    total += more;
+    return fit(e, N, by, beyond, fitted, unfit);
   }
   // The weights.  N: of values, over the largest so far and times 2^7; odd: some are hidden, and some N are not finite.
   __device__ __forceinline__ void weights(const float (&x)[16], const float (&e)[16], const f32x4 (&N)[4], bool odd) {
@@ -737,10 +850,10 @@ struct TallRows {
 
   // A lane has coefficients (8 (i / 4) + 4 half + i % 4) DT + t of its row: a record, or where there are no splits the result, by way of the
   // wave's room in LDS.
-  __device__ __forceinline__ void store(const AttendCall& a, const Part& part, uint32_t first_row, float* staged, int c, int half) {
+  __device__ __forceinline__ void store(const AttendCall& a, const Part& part, uint32_t first_row, float* staged, int c, int half, int own) {
     const float l = total + __shfl_xor(total, 32);
     const float top = l != l ? 0.f : -minus_top;         // a row that sees a NaN is one, also where it sees nothing else
-    const float unit = widest * (kValueUnit / (128.f * 127.f));
+    const float unit = __builtin_amdgcn_ldexpf(widest * (kValueUnit / (128.f * 127.f)), -own);
     const bool there = first_row + c < part.rows;
     const uint32_t row = there ? first_row + c : part.rows - 1, token = row / uint32_t(a.groups);
     const int64_t place = (part.first + token) * a.q_heads + int64_t(part.head) * a.groups + (row - token * uint32_t(a.groups));
@@ -837,7 +950,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
   auto& operands = reinterpret_cast<Stages*>(memory)->operands;
   auto& keys = reinterpret_cast<Stages*>(memory)->keys;
   __shared__ alignas(16) float scale_of[2][2][64];           // keys, values (over the largest so far, times 2^7)
-  __shared__ float2 reach[2];                    // the largest N of values so far, up to the next power of two; not 0: some N is not finite
+  __shared__ float2 reach[2];                    // the largest N of values so far, up to the next power of two; 1: some N is not finite, 2: some is beyond
+  __shared__ Fitting fitted[256];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, half = lane >> 5;
   Part part;
@@ -852,7 +966,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
     const int end = part.split == a.n_splits - 1 || start + a.chunk > all.to ? all.to : int(start + a.chunk);
     const uint32_t own = first + wave * 32;
     const int at_first = this_lane();
-    rows.begin(a, part, own, at_first & 31, at_first >> 5);
+    bool unfit = false;                      // some row's weights have a factor of its own, or may need one
+    rows.begin(a, part, own, at_first & 31, at_first >> 5, fitted + threadIdx.x);
     const Range sees(a, part, own < part.rows ? own : first, own < part.rows ? (part.rows - own < 32 ? part.rows - own : 32) : 1);
     if (begin < end) {
       const int32_t* table = a.table + part.seq * a.table_stride;
@@ -898,14 +1013,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
           const float N = (there >> lane) & 1 ? N_next : 0.f;
           const bool finite = fabsf(N) < __builtin_huge_valf();
           const float wide = wave_max(finite ? fabsf(N) : 0.f);
-          if (wide > widest) {
-            // the next power of two, within the range whose reciprocal is a normal number
-            const uint32_t up = (__float_as_uint(wide) + 0x7fffffu) & 0x7f800000u;
-            widest = __uint_as_float(up > 0x7e000000u ? 0x7e000000u : up < 0x04000000u ? 0x04000000u : up);
-          }
+          if (wide > widest) widest = wide_unit(wide);
           scale_of[buffer][1][lane] = widest > 0.f ? N * (128.f / widest) : N;
           const bool odd = __any(!finite);
-          if (lane == 0) reach[buffer] = make_float2(widest, odd ? 1.f : 0.f);
+          if (lane == 0) reach[buffer] = make_float2(widest, (odd ? 1.f : 0.f) + (wide > widest ? 2.f : 0.f));
         }
       };
       const auto load_keys = [&](const Stage& stage) {
@@ -928,7 +1039,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
       };
       // A step: its weights and weighted values, and meanwhile the products of the next one (of keys 32 next_b .. of a buffer), so that
       // the matrix cores have work while exponentials are taken.
-      const auto step = [&](i32x16& acc, int at, int buffer, int b, int next_keys, int next_b, uint32_t there, bool odd) {
+      const auto step = [&](i32x16& acc, int at, int buffer, int b, int next_keys, int next_b, uint32_t there, bool odd, float shrink, bool renew, bool beyond) {
         const bool whole = at >= sees.all_from && at + 32 <= sees.all_to && there == ~0u;
         f32x4 key_N[4], N[4];
         i32x4 key[KS];
@@ -940,13 +1051,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
         for (int g = 0; g < 4; ++g) N[g] = *reinterpret_cast<const f32x4*>(&scale_of[buffer][1][32 * b + 8 * g + 4 * half]);
         rows.scores(acc, key_N, at, whole, there, half, x);
         rows.products_high(key, acc);
-        const float more = rows.exponentials(x, rows.minus_top, e);
+        float more = rows.exponentials(x, rows.minus_top, e);
 #pragma unroll
         for (int s = 0; s < KS; ++s) {       // a product, then a share of the exponentials
           __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
           __builtin_amdgcn_sched_group_barrier(0x002, 48 / KS, 0);
         }
-        rows.refer(x, e, more);
+        if (__any(!(more <= 256.f)) || renew || unfit) unfit = rows.refer(x, e, more, N, shrink, beyond, fitted + threadIdx.x, unfit);
+        rows.total += more;
         u32x4 tile[DT];
 #pragma unroll
         for (int t = 0; t < DT; ++t) tile[t] = operands[buffer][2 * b][t][lane];
@@ -982,16 +1094,20 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
       for (int stage = begin; stage < end; stage += 64) {
         const int next_buffer = key_buffer == 2 ? 0 : key_buffer + 1, free_buffer = next_buffer == 2 ? 0 : next_buffer + 1;
         const float2 reached = reach[buffer];
-        if (reached.x > rows.widest) rows.widen(reached.x);
-        const bool odd = reached.y != 0.f;
+        const bool wider = reached.x > rows.widest, beyond = reached.y >= 2.f, odd = reached.y != 0.f && reached.y != 2.f;
+        float shrink = 1.f;                  // the values' largest N so far is another one, by whose share the sums shrink
+        if (wider) {
+          shrink = rows.widest / reached.x;
+          rows.widest = reached.x;
+        }
         const uint64_t there = now.there;
         now = after;
         load_values_of(now);
         after.find(a, part, page, stage + 128, end, lane);
         load_keys(after);
         look_up(stage + 192);
-        step(acc, stage, buffer, 0, key_buffer, 1, uint32_t(there), odd);
-        step(acc, stage + 32, buffer, 1, next_buffer, 0, uint32_t(there >> 32), odd);
+        step(acc, stage, buffer, 0, key_buffer, 1, uint32_t(there), odd, shrink, wider || beyond, beyond);
+        step(acc, stage + 32, buffer, 1, next_buffer, 0, uint32_t(there >> 32), odd, 1.f, beyond, beyond);
         buffer ^= 1;
         key_buffer = next_buffer;
         put_keys(free_buffer);
@@ -1000,7 +1116,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
       }
     }
     const int at_end = this_lane();
-    rows.store(a, part, own, reinterpret_cast<float*>(memory) + wave * kRoom, at_end & 31, at_end >> 5);
+    rows.store(a, part, own, reinterpret_cast<float*>(memory) + wave * kRoom, at_end & 31, at_end >> 5, unfit ? fitted[threadIdx.x].own : 0);
   }
 }
 

@@ -1,0 +1,117 @@
+"""Attention over the paged cache where lines differ widely in size: every finite line, seen or not, leaves the rows what the definition says.
+
+Tolerances are those of test_gpu_cache.py's check of a row, in which the weights' rounding is relative to what the row itself sees: sum_j p_j |v_j|.
+Multiplying all N by a power of two is exact, and so is taking it off the results again.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2406_11209_amd.cache import PagedCache
+from test_gpu_cache import FLOATS, check_attend, deal, filled, starts_of
+
+pytestmark = [pytest.mark.gpu, pytest.mark.timeout(300)]
+
+# dim, heads, groups, page, work, length, new tokens, max_length: rows by the few and by the many, one and several splits of the positions
+SHAPES = [
+    (128, 2, 4, 64, "f32", 200, 1, 0),              # 4 rows
+    (128, 1, 1, 16, "bf16", 1500, 1, 0),
+    (32, 1, 4, 16, "f32", 300, 9, 0),               # two tiles of rows
+    (64, 1, 3, 32, "f32", 130, 20, 0),
+    (32, 2, 4, 16, "bf16", 200, 100, 0),            # every wave with rows of its own
+    (128, 1, 4, 64, "f32", 400, 100, 0),
+    (128, 1, 2, 16, "f32", 257, 257, 64),           # positions not split
+    (64, 2, 2, 16, "bf16", 3000, 120, 0),
+    (256, 1, 4, 32, "f32", 90, 40, 0),
+    (256, 1, 2, 32, "f32", 700, 3, 0),
+]
+
+
+def made(shape, seed, array):
+    dim, heads, groups, page, work, length, new, longest = shape
+    cache = filled(PagedCache(dim, heads, -(-length // page) + 1, page, work), seed, spread=False)
+    tables, table, lengths = deal(cache, [length], seed + 1)
+    g = torch.Generator(device="cuda").manual_seed(seed + 2)
+    q = torch.randn(new, heads * groups, dim, generator=g, device="cuda").to(FLOATS[array])
+    return cache, tables, table, lengths, q
+
+
+@pytest.mark.parametrize("array", ["bf16", "f16"])
+@pytest.mark.parametrize("power", [12, 16, 24, 33, 60, 118])
+@pytest.mark.parametrize("shape", SHAPES, ids=[f"{i}" for i in range(len(SHAPES))])
+def test_large_lines_that_a_row_does_not_see(shape, power, array):
+    """A value 2^power times the others': later than a row, before its window, or further than its sequence reaches."""
+    dim, heads, groups, page, work, length, new, longest = shape
+    cache, tables, table, lengths, q = made(shape, 101, array)
+    options = dict(starts=starts_of([new]), max_new=new, max_length=longest)
+
+    def grown(position):
+        cache.v_N[tables[0][position // page], :, position % page] *= 2.0 ** power
+
+    def shrunk(position):
+        cache.v_N[tables[0][position // page], :, position % page] *= 2.0 ** -power
+
+    if new > 1:                                                          # seen by the last rows only
+        own = new - max(1, new // 3)
+        at = length - new + own
+        grown(at)
+        out = cache.attend(q, table, lengths, **options)
+        check_attend(cache, q[:own], out[:own], None, tables, [at], [own])
+        shrunk(at)
+    window = max(3, min(length - new, 100))                             # seen by no row, or by the first ones
+    at = length - new - window
+    if at >= 0:
+        grown(at)
+        out = cache.attend(q, table, lengths, window=window, **options)
+        check_attend(cache, q, out, None, tables, [length], [new], window=window)
+        shrunk(at)
+    if new > 2:
+        at = length - new - window + 1 + new // 2                        # the first half of the rows sees it
+        if 0 <= at < length - new:
+            grown(at)
+            out = cache.attend(q, table, lengths, window=window, **options)
+            last = slice(new - (new - new // 2 - 1), new)
+            check_attend(cache, q[last], out[last], None, tables, [length], [last.stop - last.start], window=window)
+            shrunk(at)
+    if length % page:                                                    # behind the end, in the last page
+        grown(length)
+        out = cache.attend(q, table, lengths, **options)
+        check_attend(cache, q, out, None, tables, [length], [new])
+
+
+@pytest.mark.parametrize("array", ["bf16", "f16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=[f"{i}" for i in range(len(SHAPES))])
+def test_large_lines_of_vanishing_weight(shape, array):
+    """A value 2^40 times the others' that every row sees, its key's score 2^-100 or less of the others' weights; and a value of zeros whose score is far
+    ahead, beside which the others are all that counts."""
+    dim, heads, groups, page, work, length, new, longest = shape
+    for far, v_power in ((-120.0, 2.0 ** 40), (30.0, 0.0)):
+        cache, tables, table, lengths, q = made(shape, 111, array)
+        q[..., :] = 1 / math.sqrt(dim)                                   # coefficient 0 is 1 under the DCT, the others 0
+        cache.k_F.fill_(0)
+        cache.k_F[..., 0] = 127
+        cache.k_N.fill_(1.0)
+        for position in (0, (length - new) // 2):
+            at = (tables[0][position // page], slice(None), position % page)
+            cache.k_F[at + (0,)] = 127 if far > 0 else -127
+            cache.k_N[at] = abs(far)
+            cache.v_N[at] *= v_power
+        if far > 0:
+            cache.v_N.copy_(cache.v_N.double() * 2.0 ** 40)                 # so that their sum is not a small number
+        out = cache.attend(q, table, lengths, starts=starts_of([new]), max_new=new, max_length=longest, scale=1.0)
+        own = slice(1 if length == new else 0, new)                     # (a prompt's first row sees nothing else)
+        check_attend(cache, q[own], out[own], None, tables, [length], [own.stop - own.start], scale=1.0)
+
+
+@pytest.mark.parametrize("power", [-90, -50, 30, 100, 121])
+@pytest.mark.parametrize("shape", SHAPES, ids=[f"{i}" for i in range(len(SHAPES))])
+def test_values_of_any_size(shape, power):
+    """All values 2^power times as large: the results are, too."""
+    dim, heads, groups, page, work, length, new, longest = shape
+    cache, tables, table, lengths, q = made(shape, 121, "bf16")
+    plain = cache.v_N.clone()
+    cache.v_N.copy_(plain.double() * 2.0 ** power)
+    out = cache.attend(q, table, lengths, starts=starts_of([new]), max_new=new, max_length=longest)
+    cache.v_N.copy_(plain)
+    check_attend(cache, q, out.double() * 2.0 ** -power, None, tables, [length], [new])
