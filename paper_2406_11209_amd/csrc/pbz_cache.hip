@@ -10,6 +10,8 @@ namespace pbz {
 namespace {
 
 constexpr int kMaxSplits = 256;
+// Workgroups of 256 threads to a launch: HIP counts a dimension's threads modulo 2^32, and leaves out the others without an error.
+constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;
 constexpr int64_t kBusyWaves = 2048;         // waves that keep the chip busy: two to a SIMD
 // Pairs of pages to a launch: 3.5 KiB of its 4 KiB of arguments; twice as many where 16 bits hold a page's number.
 constexpr int kPairsPerLaunch = 448;
@@ -402,8 +404,10 @@ int plan_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_attention*
   // several rows to a workgroup); with 4096 rows that is the slower way (62 and 56).
   p->finish_rows = p->records >= 8 && p->rows < 2048 ? 1 : 64 / (c->vol / 16);
   // the kernel for many rows finds runs of 128 rows of every sequence; there are no more of them than
+  const int64_t most = kMaxBlocks / cache->heads / p->split_blocks;
+  if (!p->tall) p->row_blocks = std::max<int64_t>(1, std::min(p->row_blocks, most / a->n_seqs));      // (a workgroup takes rows in turn)
   p->units = p->tall ? a->n_tokens * groups / 128 + a->n_seqs : a->n_seqs * p->row_blocks;
-  if (p->units > INT32_MAX / cache->heads / p->split_blocks) return PBZ_ERR_SHAPE;
+  if (p->units > most || p->rows > kMaxBlocks * (4096 / c->vol) || (!p->whole() && p->rows > kMaxBlocks * p->finish_rows)) return PBZ_ERR_SHAPE;
   p->q_bytes = padded(uint64_t(p->rows) * 2 * c->vol);
   p->scale_bytes = padded(uint64_t(p->rows) * sizeof(float));
   p->state_bytes = p->whole() ? 0 : padded(uint64_t(p->rows) * p->records * sizeof(float2));
@@ -470,9 +474,10 @@ int pbz_cache_append(const pbz_codec* c, const pbz_cache* cache, int64_t n_token
   call.slots = slots;
   call.lines = n_tokens * 2 * cache->heads;
   call.type = type;
+  const int64_t lines = 256 / (c->vol / 16), blocks = (call.lines + lines - 1) / lines;
+  if (blocks > kMaxBlocks) return PBZ_ERR_SHAPE;
   c->used.store(true);
-  const int64_t lines = 256 / (c->vol / 16);
-  const dim3 grid(unsigned((call.lines + lines - 1) / lines));
+  const dim3 grid{unsigned(blocks)};
   for_line(c->transform, c->vol, [&](auto tf, auto dim) {
     k_append<decltype(tf)::value, decltype(dim)::value><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(call);
   });
