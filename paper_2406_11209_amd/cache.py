@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import threading
 from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
@@ -172,7 +173,7 @@ class PagedCache:
         for name, pool in zip(("k_N", "k_F", "v_N", "v_F"), self.pools):
             setattr(self._struct, name, api._ptr(pool))
         self.device = self.k_N.device
-        self._spaces = {}            # stream -> workspace, its bytes
+        self._own = threading.local()     # of each thread: stream -> workspace, its bytes.  (A call is several launches through it.)
         # for the native side of the calls: entry points, codec and pools, and what tensors are held against
         self._append, self._copy, self._attend = (self._lib.addresses["pbz_cache_" + name] for name in ("append", "copy_pages", "attend"))
         self._handle, self._at = self._h.value, _c.addressof(self._struct)
@@ -233,9 +234,10 @@ class PagedCache:
                 if len(self._need) < 256:
                     self._need[sizes] = need
             stream = api._stream()
-            workspace, room = self._spaces.get(stream, (None, 0))
+            spaces = self._own.__dict__
+            workspace, room = spaces.get(stream, (None, 0))
             if room < need:
-                workspace, room = self._spaces[stream] = torch.empty(need, dtype=torch.uint8, device=self.device), need
+                workspace, room = spaces[stream] = torch.empty(need, dtype=torch.uint8, device=self.device), need
         else:
             room = workspace.numel() * workspace.element_size()
         api.check(api._binding.cache_attend(self._attend, self._handle, self._at, args, workspace, room))

@@ -18,6 +18,49 @@ def attending(seed, length=300):
     return cache, tables, table, lengths
 
 
+def test_threads_on_one_stream_have_workspaces_of_their_own(monkeypatch):
+    """An attention call is several launches through its workspace, enqueued without the interpreter's lock."""
+    cache, tables, table, lengths = attending(201)
+    used, native = {}, api._binding
+
+    class Spy:
+        def __getattr__(self, name):
+            return getattr(native, name)
+
+        def cache_attend(self, entry, codec, at, args, workspace, room):
+            first = workspace.data_ptr()
+            used.setdefault(threading.get_ident(), set()).update((first, first + room - 1))
+            return native.cache_attend(entry, codec, at, args, workspace, room)
+
+    monkeypatch.setattr(api, "_binding", Spy())
+    queries = [torch.randn(2, 8, 128, device="cuda").to(torch.bfloat16) for _ in range(4)]
+    outs, meet, failed = [[None] * 20 for _ in queries], threading.Barrier(len(queries)), []
+
+    def work(i):
+        try:
+            meet.wait()
+            for n in range(20):
+                outs[i][n] = cache.attend(queries[i], table, lengths)
+        except Exception as e:          # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(queries))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
+    torch.cuda.synchronize()
+    spans = [(min(ends), max(ends)) for ends in used.values()]
+    assert len(spans) == len(queries)
+    spans.sort()
+    assert all(a[1] < b[0] for a, b in zip(spans, spans[1:])), "threads share a workspace"
+    for q, results in zip(queries, outs):
+        for out in results:
+            check_attend(cache, q, out, None, tables, [300, 200], [1, 1])
+    assert len(used) == 4
+
+
 def test_many_short_sequences_without_a_bound_of_their_runs():
     """max_new is an expectation: where none is given, all tokens, and more workgroups than a launch can have must not follow from it."""
     seqs, page = 20000, 16
