@@ -227,6 +227,8 @@ class PagedCache:
         args.max_length, args.causal, args.window = int(max_length), 1 if causal else 0, int(window)
         args.scale = 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale)
         if workspace is None:
+            if torch.cuda.is_current_stream_capturing():
+                raise ValueError("a graph's call has to be given its workspace: the cache's own is replaced when a later call needs more")
             sizes = (tokens, args.q_heads, args.n_seqs, args.max_pages, args.max_new, args.max_length, args.window, starts is None, args.type)
             need = self._need.get(sizes)
             if need is None:

@@ -61,6 +61,33 @@ def test_threads_on_one_stream_have_workspaces_of_their_own(monkeypatch):
     assert len(used) == 4
 
 
+def test_a_graph_is_given_its_workspace():
+    """A captured call keeps the workspace's address for every replay; the cache's own is replaced when a call needs more."""
+    cache, tables, table, lengths = attending(211)
+    q = torch.randn(2, 8, 128, device="cuda").to(torch.bfloat16)
+    out, space = torch.empty_like(q), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    want = cache.attend(q, table, lengths)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        cache.attend(q, table, lengths, out=out, workspace=space)
+    torch.cuda.current_stream().wait_stream(side)
+    graph, refused = torch.cuda.CUDAGraph(), None
+    with torch.cuda.graph(graph):
+        try:
+            cache.attend(q, table, lengths, out=out)
+        except ValueError as e:
+            refused = e
+        cache.attend(q, table, lengths, out=out, workspace=space)
+    assert refused is not None and "workspace" in str(refused)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        assert torch.equal(cache.attend(q, table, lengths), want)
+
+
 def test_many_short_sequences_without_a_bound_of_their_runs():
     """max_new is an expectation: where none is given, all tokens, and more workgroups than a launch can have must not follow from it."""
     seqs, page = 20000, 16
