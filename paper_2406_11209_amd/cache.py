@@ -276,7 +276,8 @@ class PagedCache:
         return len(pairs)
 
     def extend_and_append(self, sequences: Sequence[int], counts: Sequence[int], k, v) -> None:
-        """Append the next counts[b] tokens of each sequence; their rows follow one another in k and v."""
+        """Append the next counts[b] tokens of each sequence; their rows follow one another in k and v.  Where that is refused, the sequences
+        are as they were."""
         torch = api._torch()
         if len(sequences) != len(counts) or sum(counts) != k.shape[0]:
             raise ValueError("counts have to name every row of k, sequence by sequence")
@@ -292,12 +293,12 @@ class PagedCache:
                 if copy:
                     self.copy_pages([copy])      # at once: the page copied to may be copied from by the next
                 slots.append(found)
-        except api.PbzError:                     # too few pages: the sequences stay as long as they were
+            if slots:
+                self.append(k, v, torch.from_numpy(np.concatenate(slots)).to(self.device))
+        except BaseException:                    # too few pages, or lines that are refused: the sequences stay as long as they were
             for seq, length in before:
                 self.pages.truncate(seq, length)
             raise
-        if slots:
-            self.append(k, v, torch.from_numpy(np.concatenate(slots)).to(self.device))
 
     def tables(self, sequences: Sequence[int]):
         """(table, lengths) of the sequences, on the device, for `attend`."""

@@ -88,6 +88,37 @@ def test_a_graph_is_given_its_workspace():
         assert torch.equal(cache.attend(q, table, lengths), want)
 
 
+def test_a_refused_append_leaves_the_sequences_as_they_were():
+    cache = filled(PagedCache(64, 2, 12, 16), 221)
+    x = torch.randn(20, 2, 64, device="cuda").to(torch.bfloat16)
+    a, b = cache.open(), cache.open()
+    cache.extend_and_append([a, b], [15, 5], x, x)
+    c = cache.fork(a)
+    held = [p.clone() for p in cache.pools]
+    tables = {s: cache.pages.table(s).tolist() for s in (a, b, c)}
+    k = torch.randn(6, 2, 64, device="cuda").to(torch.bfloat16)
+    turned = torch.randn(6, 64, 2, device="cuda").to(torch.bfloat16).transpose(1, 2)
+    bad = [(k, k[:5]), (k, k.float()), (k.int(), k.int()), (k, k[:, :1]), (k[..., :32], k[..., :32]), (k, k.cpu()), (k, turned), (turned, k),
+           (k.reshape(6, 128), k.reshape(6, 128)), (k, None)]
+    for i, (keys, values) in enumerate(bad):
+        with pytest.raises((ValueError, AttributeError, TypeError)):
+            cache.extend_and_append([a, b, c], [1, 2, 3], keys, values)
+            pytest.fail(f"pair {i} was not refused")
+        assert [cache.length(s) for s in (a, b, c)] == [15, 5, 15], i
+    with pytest.raises(api.PbzError):
+        cache.extend_and_append([a, b, c], [2, -1, 5], k, k)
+    assert [cache.length(s) for s in (a, b, c)] == [15, 5, 15]
+    for s in (a, b, c):                                                  # what they held is where their tables say
+        page, before = cache.pages.table(s)[0], tables[s][0]
+        n = cache.length(s)
+        assert torch.equal(cache.k_F[page, :, :n], held[1][before, :, :n]) and torch.equal(cache.v_N[page, :, :n], held[2][before, :, :n])
+    cache.extend_and_append([a, b, c], [1, 2, 3], k, k)
+    assert [cache.length(s) for s in (a, b, c)] == [16, 7, 18]
+    q = torch.randn(6, 4, 64, device="cuda").to(torch.bfloat16)
+    out = cache.attend_sequences([a, b, c], [1, 2, 3], q)
+    check_attend(cache, q, out, None, [cache.pages.table(s).tolist() for s in (a, b, c)], [16, 7, 18], [1, 2, 3])
+
+
 def test_many_short_sequences_without_a_bound_of_their_runs():
     """max_new is an expectation: where none is given, all tokens, and more workgroups than a launch can have must not follow from it."""
     seqs, page = 20000, 16
