@@ -63,6 +63,7 @@ SIGNATURES = {
     "pbz_pages_compact": (_c.c_int, [_p, _p, _i64, _i64p]),
 }
 
+_ERR_PAGES = -15
 _declared = None
 
 
@@ -78,6 +79,24 @@ def _library():
             lib.addresses[name] = _c.cast(fn, _p).value
         _declared = lib
     return lib
+
+
+def _pairs(pairs) -> np.ndarray:
+    """(from, to) pages as the library takes them: contiguous int32 [n, 2]."""
+    given = np.asarray(pairs)
+    if given.dtype == np.int32 and given.ndim == 2 and given.shape[1] == 2:
+        return np.ascontiguousarray(given)
+    if given.size == 0:
+        return np.empty((0, 2), dtype=np.int32)
+    if given.dtype == object and all(isinstance(page, int) for page in given.flat):      # beyond 64 bits
+        api.check(_ERR_PAGES)
+    if given.dtype.kind not in "iu":
+        raise ValueError("pairs of pages have to be integers")
+    if given.ndim == 0 or given.size % 2 or (given.ndim > 1 and given.shape[-1] != 2):
+        raise ValueError(f"pairs of pages have to be [n, 2], not {given.shape}")
+    if given.dtype != np.int32 and (given.min() < 0 or given.max() > 2 ** 31 - 1):        # what int32 would make another page
+        api.check(_ERR_PAGES)
+    return np.ascontiguousarray(given, dtype=np.int32).reshape(-1, 2)
 
 
 class Pages:
@@ -198,7 +217,7 @@ class PagedCache:
 
     def copy_pages(self, pairs) -> None:
         """pbz_cache_copy_pages: pairs [n, 2] (from, to), on the host."""
-        pairs = np.ascontiguousarray(pairs, dtype=np.int32).reshape(-1, 2)
+        pairs = _pairs(pairs)
         if len(pairs):
             api.check(api._binding.cache_copy(self._copy, self._handle, self._at, pairs))
 

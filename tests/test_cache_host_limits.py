@@ -1,6 +1,9 @@
 """The paged cache's limits: what a launch cannot hold is refused before any device work.  No GPU."""
 import ctypes
 
+import numpy as np
+import pytest
+
 from paper_2406_11209_amd import api, cache
 from paper_2406_11209_amd.api import Codec
 from test_cache_host import FAKE, attention, geometry
@@ -26,3 +29,19 @@ def test_more_workgroups_than_a_launch_counts():
     assert workspace(narrow, geometry(), n_tokens=1 << 23, n_seqs=1 << 23, **single) == -7
     # ... whose row blocks are fewer where an expectation of the new tokens asks for more than there can be
     assert workspace(narrow, geometry(), n_tokens=1 << 20, n_seqs=1 << 20, max_new=1 << 20, max_pages=1, table_stride=1) == 0
+
+
+def test_pairs_that_int32_would_make_other_pages():
+    for pairs in (np.array([[1, 2 ** 32 + 3]]), np.array([[2 ** 32 + 1, 3]], dtype=np.uint64), np.array([[-2 ** 32 + 1, 3]]), [(2 ** 33, 1)],
+                  [(2 ** 70, 1)], np.array([[2 ** 63 + 1, 3]], dtype=np.uint64)):
+        with pytest.raises(api.PbzError) as e:
+            cache._pairs(pairs)
+        assert e.value.status == -15
+    for pairs in (np.array([[1.5, 3.0]]), [[1, 2, 3, 4, 5, 6]], np.array([[1, 2, 3], [4, 5, 6]]), [1, 2, 3], 7, [("a", "b")], [(None, 1)],
+                  np.array([[True, False]])):
+        with pytest.raises(ValueError):
+            cache._pairs(pairs)
+    for pairs, want in (([], []), (np.zeros((0, 2), np.int64), []), ([(3, 1)], [(3, 1)]), (np.array([[5, 6], [7, 8]]).T[::-1].T, [(6, 5), (8, 7)]),
+                        (np.array([1, 2, 3, 4], dtype=np.uint8), [(1, 2), (3, 4)]), ([(np.int64(9), 2)], [(9, 2)])):
+        got = cache._pairs(pairs)
+        assert got.dtype == np.int32 and got.flags.c_contiguous and got.tolist() == [list(p) for p in want]

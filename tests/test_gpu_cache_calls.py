@@ -119,6 +119,26 @@ def test_a_refused_append_leaves_the_sequences_as_they_were():
     check_attend(cache, q, out, None, [cache.pages.table(s).tolist() for s in (a, b, c)], [16, 7, 18], [1, 2, 3])
 
 
+def test_pairs_of_pages_that_are_not_what_they_seem():
+    cache = filled(PagedCache(64, 1, 8, 16), 231)
+    held = [p.clone() for p in cache.pools]
+    for pairs in (np.array([[1, 2 ** 32 + 3]]), np.array([[2 ** 32 + 1, 3]], dtype=np.uint64), np.array([[-2 ** 32 + 1, 3]]), [(2 ** 33, 1)],
+                  [(2 ** 70, 1)]):
+        with pytest.raises(api.PbzError) as e:
+            cache.copy_pages(pairs)
+        assert e.value.status == -15
+    for pairs in (np.array([[1.5, 3.0]]), [[1, 2, 3, 4, 5, 6]], np.array([[1, 2, 3], [4, 5, 6]]), [1, 2, 3], 7, [("a", "b")]):
+        with pytest.raises(ValueError):
+            cache.copy_pages(pairs)
+    for pool, before in zip(cache.pools, held):
+        assert torch.equal(pool, before)
+    cache.copy_pages([])
+    cache.copy_pages(np.zeros((0, 2), np.int64))
+    cache.copy_pages(np.array([[1, 3]], dtype=np.uint8))
+    cache.copy_pages([(np.int64(0), 2)])
+    assert torch.equal(cache.k_F[3], held[1][1]) and torch.equal(cache.k_F[2], held[1][0])
+
+
 def test_many_short_sequences_without_a_bound_of_their_runs():
     """max_new is an expectation: where none is given, all tokens, and more workgroups than a launch can have must not follow from it."""
     seqs, page = 20000, 16
