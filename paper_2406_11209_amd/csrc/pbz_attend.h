@@ -187,6 +187,9 @@ struct Part {
   }
 };
 
+// The first position that a token sees.  (The token may be before position 0, and the window as wide as 32 bits say.)
+__device__ __forceinline__ int window_from(int position, int window) { return window > 0 && position >= window ? position - window + 1 : 0; }
+
 // The positions that rows see: any of them from .. to, all of them all_from .. all_to (each cut to what there is).
 struct Range {
   int from, to, all_from, all_to;
@@ -194,9 +197,9 @@ struct Range {
     const int groups = a.groups, before = part.length - part.fresh;
     const int first_at = before + int(first_row / groups), last_at = before + int((first_row + rows - 1) / groups);
     const int window = int(a.window);
-    from = window > 0 && first_at - window + 1 > 0 ? first_at - window + 1 : 0;
+    from = window_from(first_at, window);
     to = a.causal && last_at + 1 < part.length ? last_at + 1 : part.length;
-    all_from = window > 0 ? last_at - window + 1 : 0;
+    all_from = window_from(last_at, window);
     all_to = a.causal && first_at + 1 < part.length ? first_at + 1 : part.length;
   }
 };
@@ -311,7 +314,7 @@ struct Rows {
       place[r] = there ? at : -1;
       const int position = before + int(token);
       high[r] = !there ? -1 : a.causal ? position : part.length - 1;
-      low[r] = a.window > 0 && position - int(a.window) + 1 > 0 ? position - int(a.window) + 1 : 0;
+      low[r] = window_from(position, int(a.window));
       q_scale[r] = a.space.q_scale[at];
       if (q_scale[r] == 0.f) q_scale[r] = 0x1p-100f;     // all of the row's products are zero; a hidden one stays -infinity
       const int8_t* q = a.space.q + at * (2 * D);
@@ -716,7 +719,7 @@ struct TallRows {
     const int64_t at = (part.first + token) * a.q_heads + int64_t(part.head) * a.groups + (row - token * groups);
     const int position = part.length - part.fresh + int(token);
     high = !there ? -1 : a.causal ? position : part.length - 1;
-    low = a.window > 0 && position - int(a.window) + 1 > 0 ? position - int(a.window) + 1 : 0;
+    low = window_from(position, int(a.window));
     q_scale = a.space.q_scale[at];
     if (q_scale == 0.f) q_scale = 0x1p-100f;             // all of the row's products are zero; a hidden one stays -infinity
     const int8_t* q = a.space.q + at * (2 * D) + half * 16;

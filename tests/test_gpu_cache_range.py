@@ -115,3 +115,19 @@ def test_values_of_any_size(shape, power):
     out = cache.attend(q, table, lengths, starts=starts_of([new]), max_new=new, max_length=longest)
     cache.v_N.copy_(plain)
     check_attend(cache, q, out.double() * 2.0 ** -power, None, tables, [length], [new])
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 9, 2 ** 30])
+@pytest.mark.parametrize("dim, heads, groups", [(128, 2, 2), (32, 1, 4), (64, 1, 40), (256, 1, 3), (128, 1, 16)])
+def test_windows_as_wide_as_they_come(dim, heads, groups, window):
+    """More new tokens than positions put rows before position 0; a window that reaches past everything hides nothing."""
+    for causal in (True, False):
+        lengths_, counts = [5, 0, 40, 20], [9, 3, 40, 60]
+        cache = filled(PagedCache(dim, heads, 8, 16), 141)
+        tables, table, lengths = deal(cache, lengths_, 142)
+        q = torch.randn(sum(counts), heads * groups, dim, device="cuda").to(torch.bfloat16)
+        lse = torch.empty(q.shape[:2], device="cuda")
+        out = cache.attend(q, table, lengths, starts=starts_of(counts), max_new=max(counts), causal=causal, window=window, lse=lse)
+        check_attend(cache, q, out, lse, tables, lengths_, counts, causal)
+        few = cache.attend(q[:12], table[:2], lengths[:2], starts=starts_of(counts[:2]), max_new=1, causal=causal, window=window)
+        check_attend(cache, q[:12], few, None, tables[:2], lengths_[:2], counts[:2], causal)
