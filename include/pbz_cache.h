@@ -88,7 +88,7 @@ typedef struct pbz_attention {
   const int32_t* lengths;      /* device, n_seqs */
   const int32_t* table;        /* device, row b at b * table_stride */
   int64_t table_stride;        /* >= max_pages */
-  int64_t max_pages;           /* columns of the table */
+  int64_t max_pages;           /* columns of the table, at most 2^31 - 1024 positions */
   int64_t max_new;             /* what the longest run of new tokens is expected to be; work is dealt out by it */
   int64_t max_length;          /* likewise of lengths; 0: max_pages * page_size */
   int32_t causal;

@@ -12,6 +12,8 @@ namespace {
 constexpr int kMaxSplits = 256;
 // Workgroups of 256 threads to a launch: HIP counts a dimension's threads modulo 2^32, and leaves out the others without an error.
 constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;
+// of a sequence: the kernels look up to 256 positions ahead, in 32 bits
+constexpr int64_t kMaxPositions = (int64_t(1) << 31) - 1024;
 constexpr int64_t kBusyWaves = 2048;         // waves that keep the chip busy: two to a SIMD
 // Pairs of pages to a launch: 3.5 KiB of its 4 KiB of arguments; twice as many where 16 bits hold a page's number.
 constexpr int kPairsPerLaunch = 448;
@@ -364,7 +366,7 @@ int plan_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_attention*
   if (!a) return PBZ_ERR_NULL;
   if (a->type != PBZ_BF16 && a->type != PBZ_F16) return PBZ_ERR_TYPE;
   if (a->q_heads < 1 || a->q_heads % cache->heads || a->n_tokens < 1 || a->n_seqs < 1 || a->n_seqs > INT32_MAX ||
-      a->max_pages < 1 || a->max_pages > INT32_MAX / cache->page_size || a->table_stride < a->max_pages ||
+      a->max_pages < 1 || a->max_pages > kMaxPositions / cache->page_size || a->table_stride < a->max_pages ||
       a->table_stride > kMaxElements / a->n_seqs || a->max_new < 1 || a->max_length < 0 || a->window < 0 ||
       a->window > INT32_MAX || a->n_tokens > INT32_MAX / a->q_heads || (!a->starts && a->n_tokens != a->n_seqs))
     return PBZ_ERR_SHAPE;

@@ -45,3 +45,12 @@ def test_pairs_that_int32_would_make_other_pages():
                         (np.array([1, 2, 3, 4], dtype=np.uint8), [(1, 2), (3, 4)]), ([(np.int64(9), 2)], [(9, 2)])):
         got = cache._pairs(pairs)
         assert got.dtype == np.int32 and got.flags.c_contiguous and got.tolist() == [list(p) for p in want]
+
+
+def test_tables_whose_positions_32_bits_nearly_do_not_count():
+    """The kernels look up to 256 positions ahead; past 2^31 that was a place in front of the table."""
+    lib, need, codec = cache._library(), ctypes.c_size_t(), Codec((64,))
+    for page, most in ((16, (1 << 27) - 64), (1024, (1 << 21) - 1)):
+        for pages, status in ((most, 0), (most + 1, -7)):
+            a = attention(max_pages=pages, table_stride=pages, n_seqs=1, n_tokens=1, starts=None)
+            assert lib.pbz_cache_attend_workspace(codec._h, geometry(page_size=page), a, need) == status
