@@ -272,21 +272,6 @@ __device__ __forceinline__ void write_results(const AttendCall& a, const Part& p
   }
 }
 
-// Rows of no sequence, before the first and behind the last, are zero: a head's first workgroup sees to them.
-__device__ __forceinline__ void zero_rest(const AttendCall& a, int head, int dim) {
-  for (int side = 0; side < 2; ++side) {
-    int64_t from = side ? a.starts[a.n_seqs] : 0, to = side ? a.n_tokens : a.starts[0];
-    from = from < 0 ? 0 : from;
-    to = to > a.n_tokens ? a.n_tokens : to;
-    for (int64_t token = from; token < to; ++token)
-      for (int i = threadIdx.x; i < a.groups * dim; i += 256) {
-        const int64_t row_head = int64_t(head) * a.groups + i / dim;
-        static_cast<uint16_t*>(a.out)[token * a.out_token_stride + row_head * a.out_head_stride + i % dim] = 0;
-        if (a.lse && i % dim == 0) a.lse[token * a.q_heads + row_head] = kNegInf;
-      }
-  }
-}
-
 // A wave's 16 R rows of one head: what it keeps of them while positions go by, 32 to a step.
 template <int D, int R, bool kFine, int kN>
 struct Rows {
@@ -618,7 +603,6 @@ __global__ __launch_bounds__(256, D == 256 ? (R == 1 ? 2 : 1) : R == 1 ? 3 : 2) 
   Rows<D, R, kFine, kN> rows;
   __shared__ float left[D == 32 ? 4 : 3][Rows<D, R, kFine, kN>::kLeft * 64];      // (with more columns, at most two waves have rows)
   __shared__ float largest[4][R * 64];
-  if (a.records == 1 && a.starts && part.seq == 0 && part.row_block == 0) zero_rest(a, part.head, D);
   const uint32_t together = uint32_t(a.waves_rows) * (16 * R);
   for (uint32_t base = part.row_block * together; base < part.rows; base += a.row_blocks * together) {
     const uint32_t first = base + uint32_t(wave % a.waves_rows) * (16 * R);
@@ -958,7 +942,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const Att
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, half = lane >> 5;
   Part part;
-  if (a.records == 1 && a.starts && blockIdx.x < uint32_t(a.cache.heads)) zero_rest(a, int(blockIdx.x), D);
   if (!part.find_run(a, 128, lane)) return;
   TallRows<D, kFine> rows;
   {

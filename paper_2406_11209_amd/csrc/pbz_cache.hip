@@ -131,6 +131,14 @@ struct QueryCall {
   int32_t wide;
   float scale;             // scale log2(e) / 127
   AttendSpace space;
+  // Where nothing joins records, rows of no sequence are zeroed here, each by the lanes that have its query (by a head's first workgroup of the
+  // pass, in turn, one token beside 8191 such rows of 32 heads of 128 took 1070 us, now 46); otherwise last_bound is 0
+  void* out;
+  float* lse;
+  int64_t out_token_stride, out_head_stride;
+  const int32_t* bounds;
+  int64_t last_bound;
+  int32_t out_wide;
 };
 
 // Transformed, and held relative to the row's largest coefficient in 16 bits, +-32639 = 127 * 256 + 127, high and low byte signed.
@@ -144,6 +152,7 @@ __global__ __launch_bounds__(256) void k_queries(const QueryCall a) {
   const bool there = asked < a.rows;
   const int64_t row = there ? asked : a.rows - 1;
   const int64_t token = row / a.q_heads;
+  const int32_t begin = a.bounds[0], end = a.bounds[a.last_bound];      // of the tokens that sequences have, read before they are needed
   float v[16];
   load_run_16(a.q, a.type, token * a.token_stride + (row - token * a.q_heads) * a.head_stride + part * 16, a.wide != 0, v);
   line::forward<kTf, float, L>(v, lane);
@@ -170,6 +179,12 @@ __global__ __launch_bounds__(256) void k_queries(const QueryCall a) {
   *reinterpret_cast<uint4*>(q) = make_uint4(high[0], high[1], high[2], high[3]);
   *reinterpret_cast<uint4*>(q + D) = make_uint4(low[0], low[1], low[2], low[3]);
   if (part == 0) a.space.q_scale[row] = finite ? most * (1.f / 32639.f) * fabsf(a.scale) : __builtin_nanf("");
+  if (a.last_bound && (token < begin || token >= end)) {
+    const float none[16] = {};
+    store_run(static_cast<uint16_t*>(a.out) + token * a.out_token_stride + (row - token * a.q_heads) * a.out_head_stride + part * 16, a.type,
+              a.out_wide != 0, none);
+    if (part == 0 && a.lse) a.lse[row] = -__builtin_huge_valf();
+  }
 }
 
 struct FinishCall {
@@ -199,6 +214,11 @@ __global__ __launch_bounds__(256) void k_finish(const FinishCall a) {
   __shared__ float joined[8];
   const int64_t first = int64_t(blockIdx.x) * kRows;
   const int tid = threadIdx.x;
+  int64_t begin = 0, end = a.rows;           // of the rows that sequences have; the others' records have not been written
+  if (a.starts) {
+    begin = int64_t(a.starts[0]) * a.q_heads;
+    end = int64_t(a.starts[a.n_seqs]) * a.q_heads;
+  }
   if constexpr (kRows == 1) {
     const int column = tid % kColumns, group = tid / kColumns;
     const float* const sums = a.space.sums + first * D + column * 4;
@@ -236,7 +256,7 @@ __global__ __launch_bounds__(256) void k_finish(const FinishCall a) {
     for (int i = 0; i < 8; ++i)
       if (group + i * kGroups < a.n_splits) add(group + i * kGroups, ahead[i]);
 #pragma unroll 8
-    for (int s = group + 8 * kGroups; s < a.n_splits; s += kGroups) add(s, *reinterpret_cast<const float4*>(sums + s * apart_records));
+    for (int s = group + 8 * kGroups; s < a.n_splits && first >= begin && first < end; s += kGroups) add(s, *reinterpret_cast<const float4*>(sums + s * apart_records));
     const float by = most == kNone ? 0.f : 1.f / total;
     *reinterpret_cast<float4*>(staged + group * kPitch + column * 4) = make_float4(sum.x * by, sum.y * by, sum.z * by, sum.w * by);
     __syncthreads();
@@ -255,8 +275,9 @@ __global__ __launch_bounds__(256) void k_finish(const FinishCall a) {
         float most = kNone, total = 0.f;
 #pragma unroll 4
         for (int s = 0; s < a.n_splits; ++s) most = fmaxf(most, a.space.state[int64_t(s) * a.rows + row].x);
+        const int splits = row >= begin && row < end ? a.n_splits : 0;
 #pragma unroll 4
-        for (int s = 0; s < a.n_splits; ++s) {
+        for (int s = 0; s < splits; ++s) {
           const float2 state = a.space.state[int64_t(s) * a.rows + row];
           const float4 u = *reinterpret_cast<const float4*>(a.space.sums + (int64_t(s) * a.rows + row) * D + column * 4);
           const bool none = state.x == kNone;            // (its sums have not been written)
@@ -285,7 +306,7 @@ __global__ __launch_bounds__(256) void k_finish(const FinishCall a) {
   for (int k = 0; k < 16; ++k) v[k] = staged[in_block * kPitch + line::coefficient<kTf, L>(part, k)];
   line::inverse<kTf, float, L>(v, tid & 63);
   if (row >= a.rows) return;
-  if (a.starts && (token < a.starts[0] || token >= a.starts[a.n_seqs])) {      // a row of no sequence
+  if (row < begin || row >= end) {           // a row of no sequence
 #pragma unroll
     for (int k = 0; k < 16; ++k) v[k] = 0.f;
     if (part == 0 && a.lse) a.lse[row] = kNone;
@@ -560,6 +581,14 @@ int pbz_cache_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_atten
   query.wide = aligned(a->q) && a->q_token_stride % 8 == 0 && a->q_head_stride % 8 == 0;
   query.scale = a->scale * float(1.4426950408889634074 / 127.0);
   query.space = space;
+  query.out = a->out;
+  query.lse = a->lse;
+  query.out_token_stride = a->out_token_stride;
+  query.out_head_stride = a->out_head_stride;
+  const bool bounded = p.whole() && a->starts;
+  query.bounds = bounded ? a->starts : a->lengths;      // (any address that can be read)
+  query.last_bound = bounded ? a->n_seqs : 0;
+  query.out_wide = aligned(a->out) && a->out_token_stride % 8 == 0 && a->out_head_stride % 8 == 0;
   const dim3 query_grid(unsigned((p.rows + 256 / L - 1) / (256 / L)));
   for_line(c->transform, c->vol, [&](auto tf, auto dim) {
     k_queries<decltype(tf)::value, decltype(dim)::value><<<query_grid, 256, 0, s>>>(query);
@@ -573,7 +602,7 @@ int pbz_cache_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_atten
   call.out_head_stride = a->out_head_stride;
   call.type = a->type;
   call.transform = c->transform;
-  call.out_wide = aligned(a->out) && a->out_token_stride % 8 == 0 && a->out_head_stride % 8 == 0;
+  call.out_wide = query.out_wide;
   call.records = int32_t(p.records);
   call.starts = a->starts;
   call.lengths = a->lengths;

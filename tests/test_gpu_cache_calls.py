@@ -156,3 +156,22 @@ def test_many_short_sequences_without_a_bound_of_their_runs():
     for first in (0, 6560, 13000, seqs - 40):
         some = slice(first, first + 40)
         check_attend(cache, q[some], out[some], None, [[int(p)] for p in pages[some]], lengths[some].tolist(), [1] * 40)
+
+
+@pytest.mark.parametrize("dim, groups, length", [(128, 4, 60), (128, 4, 3000), (32, 2, 60), (64, 2, 200), (256, 3, 40)])
+def test_padded_batches(dim, groups, length):
+    """Rows of no sequence in front and behind, many of them, are zero, and nothing beside them is written."""
+    cache = filled(PagedCache(dim, 2, -(-length // 16) + 1, 16), 251)
+    tables, table, lengths = deal(cache, [length], 252)
+    for before, new, behind in ((700, 1, 900), (0, 40, 1500), (1300, 2, 0)):
+        total = before + new + behind
+        q = torch.randn(total, 2 * groups, dim, device="cuda").to(torch.bfloat16)
+        room = torch.full((total, 2 * groups, dim + 3), 5.0, device="cuda", dtype=torch.bfloat16)
+        out, lse = room[:, :, 1:dim + 1], torch.full(q.shape[:2], 3.0, device="cuda")
+        starts = torch.tensor([before, before + new], dtype=torch.int32, device="cuda")
+        cache.attend(q, table, lengths, starts=starts, max_new=new, out=out, lse=lse)
+        for rest in (slice(0, before), slice(before + new, None)):
+            assert bool((out[rest] == 0).all()) and bool((lse[rest] == float("-inf")).all())
+        assert bool((room[:, :, 0] == 5.0).all()) and bool((room[:, :, dim + 1:] == 5.0).all())
+        own = slice(before, before + new)
+        check_attend(cache, q[own], out[own], lse[own], tables, [length], [new])
