@@ -323,15 +323,17 @@ class PagedCache:
         """(table, lengths) of the sequences, on the device, for `attend`."""
         torch = api._torch()
         lengths = [self.pages.length(s) for s in sequences]
-        width = max(1, max(-(-n // self.page_size) for n in lengths))
-        table = np.stack([self.pages.table(s, width) for s in sequences])
+        width = max([1] + [-(-n // self.page_size) for n in lengths])
+        table = np.empty((len(lengths), width), dtype=np.int32)
+        for row, s in zip(table, sequences):
+            row[:] = self.pages.table(s, width)
         return torch.from_numpy(table).to(self.device), torch.tensor(lengths, dtype=torch.int32).to(self.device)
 
     def attend_sequences(self, sequences: Sequence[int], counts: Sequence[int], q, **options):
         """Attention of the last counts[b] tokens of each sequence (appended before); rows as in extend_and_append."""
         torch = api._torch()
-        if len(sequences) != len(counts) or sum(counts) != q.shape[0]:
+        if len(sequences) != len(counts) or sum(counts) != q.shape[0] or min(counts, default=0) < 0:
             raise ValueError("counts have to name every row of q, sequence by sequence")
         table, lengths = self.tables(sequences)
         starts = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).to(self.device)
-        return self.attend(q, table, lengths, starts=starts, max_new=max(1, max(counts)), **options)
+        return self.attend(q, table, lengths, starts=starts, max_new=max(counts, default=0) or 1, **options)

@@ -139,6 +139,19 @@ def test_pairs_of_pages_that_are_not_what_they_seem():
     assert torch.equal(cache.k_F[3], held[1][1]) and torch.equal(cache.k_F[2], held[1][0])
 
 
+def test_a_batch_of_no_sequences():
+    cache = PagedCache(64, 2, 4, 16)
+    none = torch.empty(0, 2, 64, device="cuda", dtype=torch.bfloat16)
+    cache.extend_and_append([], [], none, none)
+    table, lengths = cache.tables([])
+    assert table.shape == (0, 1) and lengths.shape == (0,)
+    assert cache.attend_sequences([], [], none).shape == (0, 2, 64)
+    a = cache.open()
+    assert cache.attend_sequences([a], [0], none).shape == (0, 2, 64)
+    with pytest.raises(ValueError):
+        cache.attend_sequences([a, a], [2, -2], none)
+
+
 def test_many_short_sequences_without_a_bound_of_their_runs():
     """max_new is an expectation: where none is given, all tokens, and more workgroups than a launch can have must not follow from it."""
     seqs, page = 20000, 16
