@@ -52,11 +52,11 @@ __global__ __launch_bounds__(256) void k_append(const AppendCall a) {
   line::forward<kTf, double, L>(v, lane);
   const double N = line_max<double, L>(v);
   const bool finite = N < __builtin_huge_val();
-  // Quotients as products with a reciprocal, off by some 2^-45 at most; next to a border between two indices the quotient itself decides.  Adding
-  // 1.5 * 2^52 leaves the nearest integer in the sum's lowest bits.
+  // Quotients as products with a reciprocal, off by some 2^-45 at most; next to a border between two indices the quotient itself decides, and where N is
+  // so small that the reciprocal is infinite.  Adding 1.5 * 2^52 leaves the nearest integer in the sum's lowest bits.
   const double reciprocal = N > 0.0 && finite ? 127.0 / N : 0.0;
   int r[16];
-  bool close = false;
+  bool close = !(reciprocal < __builtin_huge_val());
 #pragma unroll
   for (int k = 0; k < 16; ++k) {
     v[k] = finite ? v[k] : 0.0;

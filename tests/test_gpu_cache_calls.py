@@ -171,6 +171,18 @@ def test_many_short_sequences_without_a_bound_of_their_runs():
         check_attend(cache, q[some], out[some], None, [[int(p)] for p in pages[some]], lengths[some].tolist(), [1] * 40)
 
 
+def test_lines_below_the_normal_range():
+    """FP64 lines whose largest coefficient has no finite reciprocal times 127: the definition's indices all the same."""
+    cache = PagedCache(64, 1, 2, 16)
+    x = torch.randn(8, 1, 64, device="cuda", dtype=torch.float64)
+    scaled = x * 2.0 ** -1020                                           # exact, but for what falls below 2^-1074
+    cache.append(x, scaled, torch.arange(8, device="cuda"))
+    torch.cuda.synchronize()
+    far = (cache.k_F.int() - cache.v_F.int()).abs()
+    assert int(far.max()) <= 1 and float((far[0, :, :8] != 0).float().mean()) < 0.01
+    assert bool((cache.v_F[0, 0, :8].abs().amax(-1) == 127).all()) and bool((cache.v_N[0, 0, :8] == 0).all())
+
+
 @pytest.mark.parametrize("dim, groups, length", [(128, 4, 60), (128, 4, 3000), (32, 2, 60), (64, 2, 200), (256, 3, 40)])
 def test_padded_batches(dim, groups, length):
     """Rows of no sequence in front and behind, many of them, are zero, and nothing beside them is written."""
