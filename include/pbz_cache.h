@@ -69,9 +69,11 @@ int pbz_cache_copy_pages(const pbz_codec* codec, const pbz_cache* cache, int64_t
  * What is outside its bounds is not read: table entries outside the pool hide their positions, lengths beyond the table
  * are cut to it, starts to n_tokens.  Hidden positions' contents, whatever they are, do not reach the result (but for the
  * order of FP32 roundings: what weights refer to is renewed for several rows at a time); a line with an N that is not
- * finite makes the rows that see it not finite.
+ * finite makes the rows that see it not finite, and so may a key with an N of 2^97 or more (2^30 times N is a FP32 number
+ * on the way).
  * Arithmetic: a query row is transformed in FP32 and held in 16-bit fixed point relative to its largest coefficient;
- * products with F are exact in integers; scores, running maxima and sums, and the output's sums are FP32; a weight
+ * products with F are exact in integers; scores, running maxima and sums, and the output's sums are FP32 (scores have to be
+ * within +-2^22, beyond which FP32 does not tell neighbours apart, and a row may come out not finite); a weight
  * (times N) is rounded to FP16 once, or held in two FP16 parts where q and out are FP16.  The unit of that is a power of
  * two, such that a row's largest weight times N is between 1 and 2^15 (above 2^-79, where another row's N is 2^24 or
  * more): what is smaller than 2^-14 of the former is off by 2^-25 of it. */

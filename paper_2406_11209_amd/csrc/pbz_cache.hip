@@ -158,7 +158,8 @@ __global__ __launch_bounds__(256) void k_queries(const QueryCall a) {
   line::forward<kTf, float, L>(v, lane);
   const float most = line_max<float, L>(v);
   const bool finite = most < __builtin_huge_valf();
-  float up = finite && most > 0.f ? 32639.f / most : 0.f;
+  const float scale = finite ? most * (1.f / 32639.f) * fabsf(a.scale) : __builtin_nanf("");
+  float up = scale > 0.f ? 32639.f / most : 0.f;         // a row whose scale is 0 is taken for one of zeros
   up = up < __builtin_huge_valf() ? a.scale < 0.f ? -up : up : 0.f;
   // Adding 1.5 * 2^23 leaves the nearest integer in the sum's lowest bits; and 128, for the high byte to be signed's and the low one's bit 7 the
   // other way round.
@@ -178,7 +179,7 @@ __global__ __launch_bounds__(256) void k_queries(const QueryCall a) {
   int8_t* const q = a.space.q + row * (2 * D) + part * 16;
   *reinterpret_cast<uint4*>(q) = make_uint4(high[0], high[1], high[2], high[3]);
   *reinterpret_cast<uint4*>(q + D) = make_uint4(low[0], low[1], low[2], low[3]);
-  if (part == 0) a.space.q_scale[row] = finite ? most * (1.f / 32639.f) * fabsf(a.scale) : __builtin_nanf("");
+  if (part == 0) a.space.q_scale[row] = scale;
   if (a.last_bound && (token < begin || token >= end)) {
     const float none[16] = {};
     store_run(static_cast<uint16_t*>(a.out) + token * a.out_token_stride + (row - token * a.q_heads) * a.out_head_stride + part * 16, a.type,

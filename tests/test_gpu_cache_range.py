@@ -117,6 +117,24 @@ def test_values_of_any_size(shape, power):
     check_attend(cache, q, out.double() * 2.0 ** -power, None, tables, [length], [new])
 
 
+@pytest.mark.parametrize("power", [-90, 60, 95])
+@pytest.mark.parametrize("shape", SHAPES, ids=[f"{i}" for i in range(len(SHAPES))])
+def test_keys_of_any_size(shape, power):
+    """Keys 2^power times as large and queries as much smaller: the same scores; and a scale of 0, by which all weights are alike."""
+    dim, heads, groups, page, work, length, new, longest = shape
+    cache, tables, table, lengths, q = made(shape, 131, "bf16")
+    plain = cache.k_N.clone()
+    cache.k_N.copy_(plain.double() * 2.0 ** power)
+    small = (q.double() * 2.0 ** -power).to(q.dtype)
+    lse = torch.empty(q.shape[:2], device="cuda")
+    options = dict(starts=starts_of([new]), max_new=new, max_length=longest)
+    out = cache.attend(small, table, lengths, lse=lse, **options)
+    none = cache.attend(q, table, lengths, scale=0.0, **options)
+    cache.k_N.copy_(plain)
+    check_attend(cache, q, out, lse, tables, [length], [new])
+    check_attend(cache, q, none, None, tables, [length], [new], scale=0.0)
+
+
 @pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 9, 2 ** 30])
 @pytest.mark.parametrize("dim, heads, groups", [(128, 2, 2), (32, 1, 4), (64, 1, 40), (256, 1, 3), (128, 1, 16)])
 def test_windows_as_wide_as_they_come(dim, heads, groups, window):
