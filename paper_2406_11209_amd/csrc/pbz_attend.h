@@ -494,7 +494,7 @@ struct Rows {
   // What a wave leaves for another with the same rows: per lane references, totals, sums in one unit; the lanes of a wave side by side.
   static constexpr int kLeft = R * (2 + 4 * DT);
   __device__ __forceinline__ float unit_of(int r, const float* largest, bool unfit) const {
-    return __builtin_amdgcn_ldexpf(widest * (kValueUnit / (128.f * 127.f)), unfit ? -fitting(largest[64 * r]) : 0);
+    return __builtin_amdgcn_ldexpf(widest * (kValueUnit / (128.f * 127.f)) / kSumUnit, unfit ? -fitting(largest[64 * r]) : 0);
   }
   __device__ __forceinline__ void leave(float* left, int lane, const float* largest, bool unfit) const {
 #pragma unroll
@@ -543,7 +543,7 @@ struct Rows {
       if (l != l) top[r] = 0.f;            // a row that sees a NaN is one, also where it sees nothing else
       if (a.records == 1) {
         if (a.lse && quarter == 0 && place[r] >= 0) a.lse[place[r]] = (top[r] + __builtin_amdgcn_logf(l)) * 0.693147180559945309f;
-        const float by = top[r] == kNegInf ? 0.f : 1.f / l;
+        const float by = top[r] == kNegInf ? 0.f : kSumUnit / l;
         float* to = staged + c * kResultPitch<D> + quarter * 4 * DT;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -840,13 +840,13 @@ struct TallRows {
   __device__ __forceinline__ void store(const AttendCall& a, const Part& part, uint32_t first_row, float* staged, int c, int half, int own) {
     const float l = total + __shfl_xor(total, 32);
     const float top = l != l ? 0.f : -minus_top;         // a row that sees a NaN is one, also where it sees nothing else
-    const float unit = __builtin_amdgcn_ldexpf(widest * (kValueUnit / (128.f * 127.f)), -own);
+    const float unit = __builtin_amdgcn_ldexpf(widest * (kValueUnit / (128.f * 127.f)) / kSumUnit, -own);
     const bool there = first_row + c < part.rows;
     const uint32_t row = there ? first_row + c : part.rows - 1, token = row / uint32_t(a.groups);
     const int64_t place = (part.first + token) * a.q_heads + int64_t(part.head) * a.groups + (row - token * uint32_t(a.groups));
     if (a.records == 1) {
       if (a.lse && half == 0 && there) a.lse[place] = (top + __builtin_amdgcn_logf(l)) * 0.693147180559945309f;
-      const float by = top == kNegInf ? 0.f : unit / l;
+      const float by = top == kNegInf ? 0.f : unit * (kSumUnit / l);
 #pragma unroll 1
       for (int pass = 0; pass < 2; ++pass) {
         if (c / 16 == pass) {

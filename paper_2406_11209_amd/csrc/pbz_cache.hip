@@ -258,7 +258,7 @@ __global__ __launch_bounds__(256) void k_finish(const FinishCall a) {
       if (group + i * kGroups < a.n_splits) add(group + i * kGroups, ahead[i]);
 #pragma unroll 8
     for (int s = group + 8 * kGroups; s < a.n_splits && first >= begin && first < end; s += kGroups) add(s, *reinterpret_cast<const float4*>(sums + s * apart_records));
-    const float by = most == kNone ? 0.f : 1.f / total;
+    const float by = most == kNone ? 0.f : kSumUnit / total;
     *reinterpret_cast<float4*>(staged + group * kPitch + column * 4) = make_float4(sum.x * by, sum.y * by, sum.z * by, sum.w * by);
     __syncthreads();
     if (tid < D) {
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(256) void k_finish(const FinishCall a) {
           sum.z += none ? 0.f : f * u.z;
           sum.w += none ? 0.f : f * u.w;
         }
-        const float by = most == kNone ? 0.f : 1.f / total;
+        const float by = most == kNone ? 0.f : kSumUnit / total;
         sum = make_float4(sum.x * by, sum.y * by, sum.z * by, sum.w * by);
         if (column == 0 && a.lse) a.lse[row] = (most + __builtin_amdgcn_logf(total)) * 0.693147180559945309f;
       }

@@ -18,12 +18,15 @@ struct CacheGeom {
   const int8_t* v_F;
 };
 
+// Sums of values whose mean is a FP32 number need not be one.
+constexpr float kSumUnit = 0x1p24f;
+
 // Workspace of an attention call, [row] = [token][query head]
 struct AttendSpace {
   int8_t* q;               // [row][2][D]: a coefficient is (256 high + low) times the row's scale
   float* q_scale;          // [row], times scale log2(e) / 127
   float2* state;           // [record][row]: running maximum (of scores in units of ln 2) and sum
-  float* sums;             // [record][row][D]: coefficients of the weighted sum; not written where the maximum is -infinity
+  float* sums;             // [record][row][D]: coefficients of the weighted sum over kSumUnit; not written where the maximum is -infinity
 };
 
 struct AttendCall {

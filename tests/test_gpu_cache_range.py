@@ -149,3 +149,16 @@ def test_windows_as_wide_as_they_come(dim, heads, groups, window):
         check_attend(cache, q, out, lse, tables, lengths_, counts, causal)
         few = cache.attend(q[:12], table[:2], lengths[:2], starts=starts_of(counts[:2]), max_new=1, causal=causal, window=window)
         check_attend(cache, q[:12], few, None, tables[:2], lengths_[:2], counts[:2], causal)
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=[f"{i}" for i in range(len(SHAPES))])
+def test_sums_of_values_near_the_end_of_the_range(shape):
+    """Values whose mean FP32 holds, and whose sum it does not."""
+    dim, heads, groups, page, work, length, new, longest = shape
+    cache, tables, table, lengths, q = made(shape, 151, "bf16")
+    cache.v_F.fill_(0)
+    cache.v_F[..., 1] = torch.randint(90, 127, cache.v_F.shape[:-1], device="cuda").to(torch.int8)
+    cache.v_N.fill_(2.0 ** 125)
+    out = cache.attend(q * 0.1, table, lengths, starts=starts_of([new]), max_new=new, max_length=longest)
+    cache.v_N.fill_(1.0)
+    check_attend(cache, q * 0.1, out.double() * 2.0 ** -125, None, tables, [length], [new])
