@@ -75,7 +75,7 @@ int pbz_cache_copy_pages(const pbz_codec* codec, const pbz_cache* cache, int64_t
  * products with F are exact in integers; scores, running maxima and sums, and the output's sums are FP32 (scores have to be
  * within +-2^22, beyond which FP32 does not tell neighbours apart, and a row may come out not finite); a weight
  * (times N) is rounded to FP16 once, or held in two FP16 parts where q and out are FP16.  The unit of that is a power of
- * two, such that a row's largest weight times N is between 1 and 2^15 (above 2^-79, where another row's N is 2^24 or
+ * two, such that a row's largest weight times N is between 1 and 2^15 (above 2^-71, where another row's N is 2^32 or
  * more): what is smaller than 2^-14 of the former is off by 2^-25 of it. */
 typedef struct pbz_attention {
   const void* q;               /* device, element (t, g, d) at t * q_token_stride + g * q_head_stride + d */

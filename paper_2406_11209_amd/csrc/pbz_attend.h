@@ -36,19 +36,20 @@ constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kSlack = 8.f;          // by how much (in log2) a score may pass the maximum that the weights refer to
 
 // N of values is taken relative to the next power of two of the largest so far, between these: what a row's own factor does not reach (below) is then
-// 2^-79 and less, whatever N other rows see.
-constexpr uint32_t kLeastWide = 0x33800000u, kMostWide = 0x4b800000u;      // 2^-24, 2^24
+// 2^-71 and less, whatever N other rows see.
+constexpr uint32_t kLeastWide = 0x33800000u, kMostWide = 0x4f800000u;      // 2^-24, 2^32
 __device__ __forceinline__ float wide_unit(float wide) {
   const uint32_t up = (__float_as_uint(wide) + 0x7fffffu) & 0x7f800000u;
   return __uint_as_float(up > kMostWide ? kMostWide : up < kLeastWide ? kLeastWide : up);
 }
 
 // The exponent of a row's own factor, by its largest weight so far (or less): none from 1 to 2^15, where what is below FP16's normal numbers is off by
-// 2^-25 of the largest at most.  Otherwise the largest becomes 2^10.
+// 2^-25 of the largest at most.  Otherwise the largest becomes 2^10, or 2^14 where it is more, so that a row's total, which has the factor, too, keeps what
+// weights of 2^-29 add to it.
 __device__ __forceinline__ int fitting(float largest) {
   if (largest == 0.f || (largest >= 1.f && largest <= 32768.f)) return 0;
-  const int up = 10 + 127 - int(__float_as_uint(largest) >> 23);
-  return up > 96 ? 96 : up;
+  const int exponent = int(__float_as_uint(largest) >> 23) - 127;
+  return exponent > 0 ? 14 - exponent : exponent < -86 ? 96 : 10 - exponent;
 }
 
 // N of four neighbouring positions, as stored
@@ -407,9 +408,10 @@ struct Rows {
       const float had = unfit ? largest[64 * r] : 0.f, has = m < __builtin_huge_valf() ? m : had;      // (infinite: so is the row's result)
       largest[64 * r] = has;
       const int now = fitting(has);
-      const float by = __builtin_amdgcn_ldexpf(1.f, now - fitting(had));
+      const int change = now - fitting(had);
+      const float by = __builtin_amdgcn_ldexpf(1.f, change);       // (0 below 2^-126: so much less is what the sums held)
       if (top[r] != kNegInf) reference[r] = top[r] - float(now);
-      total[r] *= by;
+      total[r] = __builtin_amdgcn_ldexpf(total[r], change);
 #pragma unroll
       for (int t = 0; t < DT; ++t) sum[r][t] *= by;
       // (a row that has seen nothing but N of zero may come to need a factor without its reference changing)

@@ -162,3 +162,21 @@ def test_sums_of_values_near_the_end_of_the_range(shape):
     out = cache.attend(q * 0.1, table, lengths, starts=starts_of([new]), max_new=new, max_length=longest)
     cache.v_N.fill_(1.0)
     check_attend(cache, q * 0.1, out.double() * 2.0 ** -125, None, tables, [length], [new])
+
+
+@pytest.mark.parametrize("low, high, share", [(-70, 100, 1.0), (-70, 100, 0.03), (-30, 60, 0.3), (10, 40, 0.1)])
+@pytest.mark.parametrize("shape", SHAPES, ids=[f"{i}" for i in range(len(SHAPES))])
+def test_lines_of_every_size(shape, low, high, share):
+    """Values of any size between 2^low and 2^high among others of one, and some of zero, in any order, all of them seen."""
+    dim, heads, groups, page, work, length, new, longest = shape
+    cache, tables, table, lengths, q = made(shape, 161, "bf16")
+    g = torch.Generator(device="cuda").manual_seed(162)
+    powers = torch.randint(low, high + 1, cache.v_N.shape, generator=g, device="cuda").double()
+    drawn = torch.rand(powers.shape, generator=g, device="cuda") < share
+    lse = torch.empty(q.shape[:2], device="cuda")
+    plain = cache.v_N.clone()
+    for others in (low, high):
+        cache.v_N.copy_(plain.double() * torch.exp2(torch.where(drawn, powers, float(others))))
+        cache.v_N[torch.rand(powers.shape, generator=g, device="cuda") < 0.1] = 0
+        out = cache.attend(q, table, lengths, starts=starts_of([new]), max_new=new, max_length=longest, lse=lse)
+        check_attend(cache, q, out, lse, tables, [length], [new])
