@@ -45,7 +45,8 @@ int pbz_cache_layout(const pbz_codec* codec, const pbz_cache* cache, size_t* n_b
  * rounded once, to the working type.  A line with a NaN or an infinity in it gives N = NaN, F = 0.
  *   k, v      device, element (t, h, d) at t * token_stride + h * head_stride + d; strides in elements, >= 0.  Any
  *             alignment of the element type; loads are wide where base and strides are multiples of 16 bytes.
- *   slots     device, n_tokens; a slot outside the pool (-1, say) leaves its token out.  Two tokens with one slot race. */
+ *   slots     device, n_tokens; a slot outside the pool (-1, say) leaves its token out.  Two tokens with one slot race.
+ * More lines than a launch of 2^24 - 1 workgroups of 4096 / D takes are refused (PBZ_ERR_SHAPE), and likewise rows of q. */
 typedef struct pbz_lines {
   const void* data;
   int64_t token_stride;

@@ -228,7 +228,8 @@ class PagedCache:
         table [sequences, pages] and lengths [sequences], int32; starts [sequences + 1] int32, the rows of each
         sequence's new tokens (None: one token a sequence).  max_new, max_length: the host's bounds of the runs of new
         tokens and of the lengths, by which the work is dealt out (defaults: all tokens; the table's width).
-        lse: float32 [tokens, query heads], written.  scale: 1 / sqrt(head_dim) when None."""
+        lse: float32 [tokens, query heads], written.  scale: 1 / sqrt(head_dim) when None.  workspace: the cache's own, one for every
+        thread and stream, when None; a call that is captured into a graph has to be given one."""
         if q.dim() != 3:
             raise ValueError("q has to be [tokens, query heads, head_dim]")
         torch = api._torch()

@@ -15,7 +15,8 @@
 //   range    The largest N so far may be of a line that a row does not see, or sees with no weight, and then all of its weights would be
 //            lost in FP16.  So it is checked that each row has a weight of 1 at least, where the references or the largest N change, which is
 //            seldom.  While some row has none, the rows' largest weights are found at every step, and such rows have a factor of their own, a
-//            power of two.  The check costs a prompt 0.5 % (712 -> 715 us), a single token of 300 positions 6 % (10.9 -> 11.6 us).
+//            power of two.  The check costs a prompt 0.5 % (712 -> 715 us), a single token of 300 positions 6 % (10.9 -> 11.6 us: code that is read
+//            once); as one branch with the change that asks for it, and with nothing held in registers for it in the usual steps.
 // Lanes 16 apart share a position's line: a line of 128 is one 128-byte read of 8 (keys) or 16 lanes (values).
 #pragma once
 
@@ -922,9 +923,9 @@ struct Stage {
 // converts the values of 16 of them into LDS, where every wave finds its operands, and N of all lies there, too; two buffers, so one
 // barrier to a stage.  Every load is made whether or not it will be used (behind the end: of the pool's first line), so that
 // the waits between loads and their uses count exactly.
-// Bound by vector instructions, of which there are 220 to 32 positions of 32 rows of 128, 16 of them exponentials at a quarter of the rate; they
-// are issued in 71 % of the time, and the matrix cores are busy in 38 %.  A prompt of 8192, 32 query heads on 8 of 128: 690 to 780 us on different
-// cards, 0.7 to 0.8 PFLOP/s.  (Wave by wave with tiles of 16, as k_attend: 1022 us.)
+// Bound by vector instructions, of which there are 223 to 32 positions of 32 rows of 128, 16 of them exponentials at a quarter of the rate; they
+// are issued in 71 % of the time, and the matrix cores are busy in 38 %.  A prompt of 8192, 32 query heads on 8 of 128: 680 to 740 us on different
+// cards, 0.74 to 0.8 PFLOP/s.  (Wave by wave with tiles of 16, as k_attend: 1022 us.)
 template <int D, bool kFine, int kN>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tall(const AttendCall a) {
   constexpr int DT = D / 32, KS = D / 32, VW = D >= 128 ? D / 128 : 1;

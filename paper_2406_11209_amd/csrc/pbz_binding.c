@@ -268,7 +268,7 @@ static PyObject *segmented(PyObject *self, PyObject *const *args, Py_ssize_t n) 
 }
 
 /* ---- the paged compressed cache (paper_2406_11209_amd/cache.py): an append took 6.3 us of host time with ctypes, an attention call of two launches 11.7,
- * a copy of a few pages 5.1; now 4.0, 8.9 and 3.5 ---- */
+ * a copy of a few pages 5.1; now 4.0, 9.5 and 3.5 ---- */
 
 /* What a cache's tensors are held against: PyTuple (device, int32, int64, float32, heads, head_dim) */
 enum { kDevice, kInt32, kInt64, kFloat32, kHeads, kDim, kOfCache };

@@ -30,8 +30,8 @@ struct AppendCall {
 };
 
 // L = D / 16 lanes to a line; a wave's indices go through LDS, where a lane's coefficients, L apart, become 16 neighbouring bytes.
-// Bound by FP64 instructions: 8192 tokens of 8 heads of 128 take 26.8 us (1.9 TB/s), of which 21 are their issue (800 to a wave's 8 lines).  64
-// tokens take 4.3 us, a launch's latencies.
+// Bound by FP64 instructions: 8192 tokens of 8 heads of 128, bfloat16, take 26 us (2.0 TB/s), of which 21 are their issue (800 to a wave's 8 lines).  64
+// tokens take 4.7 us, a launch's latencies.
 template <int kTf, int D>
 __global__ __launch_bounds__(256) void k_append(const AppendCall a) {
   constexpr int L = D / 16, kLines = 64 / L, kPitch = D + 4;      // the pitch keeps lines off one bank
@@ -142,7 +142,7 @@ struct QueryCall {
 };
 
 // Transformed, and held relative to the row's largest coefficient in 16 bits, +-32639 = 127 * 256 + 127, high and low byte signed.
-// 262144 rows of 128: 35 us (3.8 TB/s), 30 of them the issue of its 570 instructions to a wave's 8 rows.
+// 262144 rows of 128: 37 us (3.6 TB/s), 30 of them the issue of its 573 instructions to a wave's 8 rows.
 template <int kTf, int D>
 __global__ __launch_bounds__(256) void k_queries(const QueryCall a) {
   constexpr int L = D / 16, kLines = 64 / L, kPitch = D + 2;      // in coefficients of 16 bits
@@ -202,7 +202,7 @@ struct FinishCall {
   int32_t n_splits;
 };
 
-// Joins the splits of a row, divides by the sum and transforms back.  64 records of 32 rows of 128: 5.5 us; 3 of 25408 rows: 12.4 us, 3.7 TB/s.
+// Joins the splits of a row, divides by the sum and transforms back.  64 records of 32 rows of 128: 5.5 us; 3 of 25408 rows: 12.7 us, 3.6 TB/s.
 // A launch of its own, since the caches of two dies do not see each other's stores: with the last workgroup of a unit joining its records, written
 // through to memory and read from there, the calls of those two took 76 and 127 us instead of 68 and 91.  kRows rows to a workgroup: with one, the threads share its splits;
 // with more, every thread takes four columns of a row through all of them.
@@ -412,8 +412,8 @@ int plan_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_attention*
   if (a->window > 0) length = std::min(length, a->window + fresh + 63);
   // Splits of the positions, where rows alone do not fill the chip, for 1400, 2048 and 3000 waves: chunks of 10 to 387 after up to 3528 95, 87 and 107
   // us, one token of 131072 71, 65 and 70, of 64 uneven sequences to 8200 128, 128 and 191; the tall kernel for lines of 256 has one wave to a SIMD
-  // (32 rows after 16 x 4096: 155 us with 1024, 174 with 2048).  Down to 64 positions: one token after 8000 takes 18 us, 21 with at least 128 and
-  // 23 with 256.
+  // (32 new tokens of 4 query heads, 128 rows, after 16 x 4096: 153 us with 1024, 172 with 2048; 128 new tokens after 4 x 4096 140 and 159).  Down to 64
+  // positions: one token after 8000, lines of 128, takes 18 us, 21 with at least 128 and 23 with 256.
   // (max_new bounds the tiles of every sequence, all rows together those of all)
   const int64_t some = std::min(a->n_seqs * tiles, (a->n_tokens * groups + p->tile - 1) / p->tile + a->n_seqs);
   const int64_t alone = some * cache->heads, busy = p->tall && c->vol == 256 ? kBusyWaves / 2 : kBusyWaves;
@@ -424,8 +424,8 @@ int plan_attend(const pbz_codec* c, const pbz_cache* cache, const pbz_attention*
   p->row_blocks = (tiles + p->waves_rows - 1) / p->waves_rows;
   p->split_blocks = (p->n_splits + waves_splits - 1) / waves_splits;
   p->records = p->split_blocks;
-  // Joining: few rows of many records have a workgroup each, whose threads share the records (32 rows of 131072 positions: 54 us in all, 64 with
-  // several rows to a workgroup); with 4096 rows that is the slower way (62 and 56).
+  // Joining: few rows of many records have a workgroup each, whose threads share the records (32 rows of 131072 positions, the same call over and
+  // over: 54 us in all, 64 with several rows to a workgroup); with 4096 rows of 16 records that is the slower way (58 and 52), and with 2048 (41 and 38).
   p->finish_rows = p->records >= 8 && p->rows < 2048 ? 1 : 64 / (c->vol / 16);
   // the kernel for many rows finds runs of 128 rows of every sequence; there are no more of them than
   const int64_t most = kMaxBlocks / cache->heads / p->split_blocks;
